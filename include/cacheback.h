@@ -62,8 +62,10 @@ enum {
   CB_ERR_WORKSPACE = -5, /* workspace missing or smaller than required */
   CB_ERR_ALIGN = -6,     /* device pointer not 16-byte aligned */
   CB_ERR_HIP = -7,       /* HIP launch error */
-  CB_ERR_TIMEOUT = -8    /* a dependency wait inside a kernel gave up (reported
+  CB_ERR_TIMEOUT = -8,   /* a dependency wait inside a kernel gave up (reported
                             by cb_score_status / cb_select_status) */
+  CB_ERR_PAGES = -9      /* a cache has too few free pages (cacheback_cache.h;
+                            reported by cb_cache_status) */
 };
 
 typedef enum { CB_F32 = 0, CB_BF16 = 1 } cb_dtype;

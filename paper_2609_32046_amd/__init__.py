@@ -1,7 +1,8 @@
 """MI355X receiver-conditioned KV selection: Python binding of ``libcacheback.so``.
 
 Argument marshalling only.  Every step of the path runs in the HIP kernels
-behind the C ABI declared in ``include/cacheback.h``; this module converts
+behind the C ABI declared in ``include/cacheback.h`` and
+``include/cacheback_cache.h``; this module converts
 torch tensors (or raw integer device pointers) to pointers, passes the current
 HIP stream, and turns status codes into exceptions.  torch is used for device
 memory and streams only.
@@ -20,7 +21,7 @@ LIB_PATH = os.path.join(_HERE, "libcacheback.so")
 CB_F32, CB_BF16 = 0, 1
 STATUS = {0: "CB_OK", -1: "CB_ERR_NULL", -2: "CB_ERR_SHAPE", -3: "CB_ERR_DTYPE",
           -4: "CB_ERR_RATIO", -5: "CB_ERR_WORKSPACE", -6: "CB_ERR_ALIGN", -7: "CB_ERR_HIP",
-          -8: "CB_ERR_TIMEOUT"}
+          -8: "CB_ERR_TIMEOUT", -9: "CB_ERR_PAGES"}
 
 if not os.path.exists(LIB_PATH):
     raise ImportError(
@@ -84,6 +85,53 @@ _lib.cb_select_spans.argtypes = [_vp, _i64, _i64, _i64, _i64, ctypes.c_int32, _v
 _lib.cb_select_spans.restype = ctypes.c_int
 _lib.cb_gather_rows.argtypes = [_vp, _i64, _i64, _i64, _vp, _i64, _vp, _vp]
 _lib.cb_gather_rows.restype = ctypes.c_int
+
+
+class _rope(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("scaling", ctypes.c_int32),
+                ("base", ctypes.c_double), ("factor", ctypes.c_double),
+                ("original_len", ctypes.c_double), ("fast_turns", ctypes.c_double),
+                ("slow_turns", ctypes.c_double)]
+
+
+class cb_rows(ctypes.Structure):
+    _fields_ = [("x", _vp), ("out", _vp), ("pos", _vp), ("frm", _vp), ("size", _i64 * 3),
+                ("in_stride", _i64 * 3), ("out_stride", _i64 * 3), ("pos_stride", _i64 * 3),
+                ("from_stride", _i64 * 3)]
+
+
+class cb_cache(ctypes.Structure):
+    _fields_ = [("layers", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("page_len", ctypes.c_int32),
+                ("pages", ctypes.c_int32), ("seqs", ctypes.c_int32), ("width", ctypes.c_int32),
+                ("reserved", ctypes.c_int32), ("pool", _vp), ("refs", _vp), ("table", _vp),
+                ("lens", _vp)]
+
+
+_i32, _pc = ctypes.c_int32, ctypes.POINTER(cb_cache)
+for _name, _args, _res in [
+        ("cb_rotary_frequencies", [ctypes.POINTER(_rope), _vp, ctypes.POINTER(ctypes.c_double)], ctypes.c_int),
+        ("cb_rotary", [ctypes.POINTER(cb_rows), _i32, _i32, _vp, _i32, ctypes.c_double, _i32, _i32, _i32, _vp],
+         ctypes.c_int),
+        ("cb_cache_page_bytes", [_pc], _sz),
+        ("cb_cache_status", [_vp, _vp], ctypes.c_int),
+        ("cb_cache_extend", [_pc, _vp, _vp, _i32, _vp, _vp], ctypes.c_int),
+        ("cb_cache_free", [_pc, _vp, _i32, _vp], ctypes.c_int),
+        ("cb_cache_fork_workspace_bytes", [_pc, _i32], _sz),
+        ("cb_cache_fork", [_pc, _vp, _vp, _i32, _i32, _vp, _vp, _sz, _vp], ctypes.c_int),
+        ("cb_cache_compact_workspace_bytes", [_pc, _i32], _sz),
+        ("cb_cache_compact", [_pc, _vp, _vp, _i32, _vp, ctypes.POINTER(_i64), _i64, _vp, _vp, _vp, _sz, _vp],
+         ctypes.c_int),
+        ("cb_cache_write", [_pc, _i32, _i32, _vp, _i32, _vp, _vp, _i64, _vp, _vp,
+                            ctypes.POINTER(_i64), _i32, _vp], ctypes.c_int),
+        ("cb_cache_read", [_pc, _i32, _i32, _vp, _i32, _vp, _vp, _i64, _vp, _vp,
+                           ctypes.POINTER(_i64), _i32, _vp], ctypes.c_int),
+        ("cb_cache_attend_workspace_bytes", [_pc, _i32, _i32, _i32, _i64], _sz),
+        ("cb_cache_attend", [_pc, _i32, _i32, _vp, _i32, _vp, ctypes.POINTER(_i64), _i32, _vp, _i64,
+                             _i32, ctypes.c_double, _vp, ctypes.POINTER(_i64), _vp, _i32, _vp, _sz,
+                             _vp], ctypes.c_int)]:
+    getattr(_lib, _name).argtypes = _args
+    getattr(_lib, _name).restype = _res
 _lib.cb_status_string.argtypes = [ctypes.c_int]
 _lib.cb_status_string.restype = ctypes.c_char_p
 
@@ -349,11 +397,282 @@ class PositionBuffers:
                                    device=device)
 
 
+# ---------------------------------------------------------------------------
+# The receiver's side: rotary positions, the paged four-bit cache, attention
+
+
+def _tensor(x, where, dtypes=None, ndim=None, shape=None):
+    """Checks of a tensor argument that its pointer cannot show: type, shape
+    (None: any size), and that it lies on the current device."""
+    import torch
+
+    if x.device.type != "cuda" or x.device.index != torch.cuda.current_device():
+        raise CBError(-2, f"{where}: tensor on {x.device}, not on the current device")
+    if dtypes is not None and x.dtype not in dtypes:
+        raise CBError(-3, f"{where}: {x.dtype}")
+    if ndim is not None and x.dim() != ndim:
+        raise CBError(-2, f"{where}: {x.dim()} axes, {ndim} wanted")
+    if shape is not None and (x.dim() != len(shape) or any(
+            s is not None and s != n for n, s in zip(x.shape, shape))):
+        raise CBError(-2, f"{where}: shape {tuple(x.shape)}, {tuple(shape)} wanted")
+    return x
+
+
+def _ints(x, where, n=None):
+    """A contiguous int32 list (of n entries), or None."""
+    import torch
+
+    if x is None:
+        return None
+    _tensor(x, where, (torch.int32,), 1, None if n is None else (n,))
+    if not x.is_contiguous():
+        raise CBError(-2, f"{where}: not contiguous")
+    return x
+
+
+def _dtype_of(x, where):
+    import torch
+
+    if x.dtype == torch.float32:
+        return CB_F32
+    if x.dtype == torch.bfloat16:
+        return CB_BF16
+    raise CBError(-3, f"{where}: {x.dtype}")
+
+
+def _strided(x, where):
+    """Strides of all axes but the last, whose values have to be contiguous."""
+    if x.shape[-1] > 1 and x.stride(-1) != 1:
+        raise CBError(-2, f"{where}: the values of a row are not contiguous")
+    return (_i64 * (x.dim() - 1))(*x.stride()[:-1])
+
+
+def cb_rotary_frequencies(rotary_dim: int, base: float = 10000.0, scaling: str = "none",
+                          factor: float = 1.0, original_len: float = 0.0,
+                          fast_turns: float = 0.0, slow_turns: float = 0.0):
+    """(turns per position of every pair, as a host list; amplitude).  scaling:
+    "none", "linear" or "yarn"."""
+    import array
+
+    kinds = {"none": 0, "linear": 1, "yarn": 2}
+    if scaling not in kinds:
+        raise CBError(-2, f"cb_rotary_frequencies: scaling {scaling!r}")
+    r = _rope(int(rotary_dim), kinds[scaling], float(base), float(factor), float(original_len),
+              float(fast_turns), float(slow_turns))
+    freq, amp = array.array("d", bytes(8 * max(0, min(int(rotary_dim), 1024) // 2 + 1))), ctypes.c_double(0.0)
+    _check(_lib.cb_rotary_frequencies(ctypes.byref(r), freq.buffer_info()[0], ctypes.byref(amp)),
+           "cb_rotary_frequencies")
+    return list(freq[:int(rotary_dim) // 2]), amp.value
+
+
+def rows(x, out, pos, frm=None) -> cb_rows:
+    """Rows of one tensor for cb_rotary: x and out [a][b][c][D] (out may be x), int32 positions
+    `pos` and earlier ones `frm` of shapes that broadcast to [a][b][c].  The struct keeps its
+    tensors."""
+    import torch
+
+    where = "rows"
+    _tensor(x, where, (torch.float32, torch.bfloat16), 4)
+    _tensor(out, where, (x.dtype,), 4, x.shape)
+    r = cb_rows(x=x.data_ptr(), out=out.data_ptr(), size=(_i64 * 3)(*x.shape[:3]),
+                in_stride=_strided(x, where), out_stride=_strided(out, where))
+    r.tensors = (x, out, pos, frm)
+    r.dtype, r.head_dim = _dtype_of(x, where), x.shape[3]
+    for p, name, stride in ((pos, "pos", "pos_stride"), (frm, "frm", "from_stride")):
+        if p is not None:
+            _tensor(p, where, (torch.int32,))
+            try:
+                q = p.expand(x.shape[:3])
+            except RuntimeError:
+                raise CBError(-2, f"{where}: positions {tuple(p.shape)} for rows "
+                                  f"{tuple(x.shape[:3])}") from None
+            setattr(r, name, q.data_ptr())
+            setattr(r, stride, (_i64 * 3)(*q.stride()))
+    return r
+
+
+def cb_rotary(parts, freq, amplitude: float = 1.0, interleaved: bool = False,
+              transpose: bool = False, stream=None) -> None:
+    """Rotates the rows of one or two tensors (`rows`) by the frequencies `freq` (device, float64,
+    one a pair)."""
+    import torch
+
+    parts = [parts] if isinstance(parts, cb_rows) else list(parts)
+    _tensor(freq, "cb_rotary", (torch.float64,), 1)
+    if not freq.is_contiguous():
+        raise CBError(-2, "cb_rotary: freq not contiguous")
+    if not 1 <= len(parts) <= 2:
+        raise CBError(-2, "cb_rotary: one or two tensors")
+    if any(p.dtype != parts[0].dtype or p.head_dim != parts[0].head_dim for p in parts):
+        raise CBError(-3, "cb_rotary: parts of unlike types or widths")
+    a = parts[0] if len(parts) == 1 else (cb_rows * 2)(*parts)
+    _check(_lib.cb_rotary(a if len(parts) == 2 else ctypes.byref(a), len(parts), parts[0].head_dim,
+                          freq.data_ptr(), 2 * freq.numel(), float(amplitude), int(interleaved),
+                          int(transpose), parts[0].dtype, _stream(stream)), "cb_rotary")
+
+
+def cache(pool, refs, table, lens, head_dim: int, page_len: int) -> cb_cache:
+    """Descriptor of a paged four-bit cache over the caller's tensors: pool uint8
+    [pages][layers][kv_heads][unit], int32 refs [pages], table [seqs][width], lens [seqs].  It keeps
+    them."""
+    import torch
+
+    where, D, P = "cache", int(head_dim), int(page_len)
+    _tensor(pool, where, (torch.uint8,), 4, (None, None, None, P * (D + D // 16)))
+    _tensor(refs, where, (torch.int32,), 1, (pool.shape[0],))
+    _tensor(table, where, (torch.int32,), 2)
+    _tensor(lens, where, (torch.int32,), 1, (table.shape[0],))
+    for t in (pool, refs, table, lens):
+        if not t.is_contiguous():
+            raise CBError(-2, f"{where}: not contiguous")
+    c = cb_cache(pool.shape[1], pool.shape[2], D, P, pool.shape[0], table.shape[0], table.shape[1],
+                 0, pool.data_ptr(), refs.data_ptr(), table.data_ptr(), lens.data_ptr())
+    c.tensors = (pool, refs, table, lens)
+    if _lib.cb_cache_page_bytes(ctypes.byref(c)) == 0:
+        raise CBError(-2, where)
+    return c
+
+
+class Cache:
+    """Device buffers of a paged four-bit cache (torch allocations), empty, and its descriptor
+    `desc`."""
+
+    def __init__(self, layers, kv_heads, head_dim, page_len, pages, seqs, width, device="cuda"):
+        import torch
+
+        i32 = dict(dtype=torch.int32, device=device)
+        self.pool = torch.empty((pages, layers, kv_heads, page_len * (head_dim + head_dim // 16)),
+                                dtype=torch.uint8, device=device)
+        self.refs = torch.zeros(pages, **i32)
+        self.table = torch.full((seqs, width), -1, **i32)
+        self.lens = torch.zeros(seqs, **i32)
+        self.status = torch.zeros(1, **i32)
+        self.desc = cache(self.pool, self.refs, self.table, self.lens, head_dim, page_len)
+
+
+def cb_cache_page_bytes(c: cb_cache) -> int:
+    return _lib.cb_cache_page_bytes(ctypes.byref(c))
+
+
+def cb_cache_status(status, stream=None) -> int:
+    """Synchronises the stream and returns 0 (CB_OK), -9 (CB_ERR_PAGES: pages lacked) or -2
+    (CB_ERR_SHAPE: an invalid entry) for the last call that wrote `status`."""
+    return _lib.cb_cache_status(_ptr(_ints(status, "cb_cache_status", 1)), _stream(stream))
+
+
+def cb_cache_extend(c: cb_cache, seqs, add, status, stream=None) -> None:
+    n = _ints(seqs, "cb_cache_extend").numel()
+    _check(_lib.cb_cache_extend(ctypes.byref(c), _ptr(seqs), _ptr(_ints(add, "cb_cache_extend", n)), n,
+                                _ptr(_ints(status, "cb_cache_extend", 1)), _stream(stream)),
+           "cb_cache_extend")
+
+
+def cb_cache_free(c: cb_cache, seqs, stream=None) -> None:
+    n = _ints(seqs, "cb_cache_free").numel()
+    _check(_lib.cb_cache_free(ctypes.byref(c), _ptr(seqs), n, _stream(stream)), "cb_cache_free")
+
+
+def cb_cache_fork_workspace_bytes(c: cb_cache, n: int) -> int:
+    return _lib.cb_cache_fork_workspace_bytes(ctypes.byref(c), int(n))
+
+
+def cb_cache_fork(c: cb_cache, parents, children, status, ws, copy: bool = False, ws_bytes=None,
+                  stream=None) -> None:
+    n = _ints(parents, "cb_cache_fork").numel()
+    _ints(children, "cb_cache_fork", n)
+    _check(_lib.cb_cache_fork(ctypes.byref(c), _ptr(parents), _ptr(children), n, int(copy),
+                              _ptr(_ints(status, "cb_cache_fork", 1)), _ptr(ws),
+                              _nbytes(ws, ws_bytes), _stream(stream)), "cb_cache_fork")
+
+
+def cb_cache_compact_workspace_bytes(c: cb_cache, n: int) -> int:
+    return _lib.cb_cache_compact_workspace_bytes(ctypes.byref(c), int(n))
+
+
+def cb_cache_compact(c: cb_cache, src, dst, idx, status, ws, counts=None, ws_bytes=None,
+                     stream=None) -> None:
+    """idx: int32 [n][layers or 1][kv_heads or 1][keep]; an axis of one serves all."""
+    import torch
+
+    where = "cb_cache_compact"
+    n = _ints(src, where).numel()
+    _ints(dst, where, n)
+    _ints(counts, where, n)
+    _tensor(idx, where, (torch.int32,), 4)
+    if idx.shape[3] > 1 and idx.stride(3) != 1:
+        raise CBError(-2, f"{where}: a list of positions is not contiguous")
+    try:
+        full = idx.expand(n, c.layers, c.kv_heads, idx.shape[3])
+    except RuntimeError:
+        raise CBError(-2, f"{where}: lists {tuple(idx.shape)}") from None
+    _check(_lib.cb_cache_compact(ctypes.byref(c), _ptr(src), _ptr(dst), n, _ptr(idx),
+                                 (_i64 * 3)(*full.stride()[:3]), idx.shape[3], _ptr(counts),
+                                 _ptr(_ints(status, where, 1)), _ptr(ws), _nbytes(ws, ws_bytes),
+                                 _stream(stream)), where)
+
+
+def _cache_rows(fn, where, c, k, v, seqs, start, counts, layer, stream):
+    _tensor(k, where, None, 5, (None, None, c.kv_heads, None, c.head_dim))
+    _tensor(v, where, (k.dtype,), 5, k.shape)
+    if k.stride() != v.stride():
+        raise CBError(-2, f"{where}: keys and values of unlike strides")
+    L, n, _, T, _ = k.shape
+    lists = [_ptr(_ints(x, where, n)) for x in (seqs, start, counts)]
+    _check(fn(ctypes.byref(c), int(layer), L, lists[0], n, lists[1], lists[2], T, k.data_ptr(),
+              v.data_ptr(), _strided(k, where), _dtype_of(k, where), _stream(stream)), where)
+
+
+def cb_cache_write(c: cb_cache, k, v, seqs=None, start=None, counts=None, layer: int = 0,
+                   stream=None) -> None:
+    """k, v [layers][n][kv_heads][rows][D] into the cache, from `layer` on."""
+    _cache_rows(_lib.cb_cache_write, "cb_cache_write", c, k, v, seqs, start, counts, layer, stream)
+
+
+def cb_cache_read(c: cb_cache, k, v, seqs=None, start=None, counts=None, layer: int = 0,
+                  stream=None) -> None:
+    """The cache's values into k, v [layers][n][kv_heads][rows][D]."""
+    _cache_rows(_lib.cb_cache_read, "cb_cache_read", c, k, v, seqs, start, counts, layer, stream)
+
+
+def cb_cache_attend_workspace_bytes(c: cb_cache, layers: int, n: int, q_heads: int,
+                                    q_len: int) -> int:
+    """Scratch bytes of cb_cache_attend (0: it needs none)."""
+    return _lib.cb_cache_attend_workspace_bytes(ctypes.byref(c), int(layers), int(n), int(q_heads),
+                                                int(q_len))
+
+
+def cb_cache_attend(c: cb_cache, q, out, ws=None, lse=None, seqs=None, q_lens=None,
+                    causal: bool = True, scale: float = 0.0, layer: int = 0, ws_bytes=None,
+                    stream=None) -> None:
+    """q, out [layers][n][q_heads][q_len][D]; lse [layers][n][q_heads][q_len] fp32."""
+    import torch
+
+    where = "cb_cache_attend"
+    _tensor(q, where, None, 5, (None, None, None, None, c.head_dim))
+    _tensor(out, where, (q.dtype,), 5, q.shape)
+    L, n, Hq, m, _ = q.shape
+    if lse is not None:
+        _tensor(lse, where, (torch.float32,), 4, q.shape[:4])
+        if not lse.is_contiguous():
+            raise CBError(-2, f"{where}: lse not contiguous")
+    _check(_lib.cb_cache_attend(ctypes.byref(c), int(layer), L, _ptr(_ints(seqs, where, n)), n,
+                                q.data_ptr(), _strided(q, where), Hq,
+                                _ptr(_ints(q_lens, where, n)), m, int(causal), float(scale),
+                                out.data_ptr(), _strided(out, where), _ptr(lse),
+                                _dtype_of(q, where), _ptr(ws), _nbytes(ws, ws_bytes),
+                                _stream(stream)), where)
+
+
 __all__ = ["cb_layout", "layout", "layout_of", "cb_score_workspace_bytes", "cb_score",
            "cb_keep_count", "cb_select", "cb_compact", "cb_status_string", "CBError",
            "cb_pipeline", "cb_score_status", "cb_set_wait_limit", "cb_position_workspace_bytes",
            "cb_position_score", "cb_position_status", "cb_budget_fanout", "cb_budget_chain",
            "cb_spans_workspace_bytes", "cb_select_spans", "cb_gather_rows", "PositionBuffers",
            "cb_pipeline_noalloc", "cb_select_workspace_bytes", "cb_select_ws", "cb_select_status",
+           "cb_rotary_frequencies", "cb_rows", "rows", "cb_rotary", "cb_cache", "cache", "Cache",
+           "cb_cache_page_bytes", "cb_cache_status", "cb_cache_extend", "cb_cache_free",
+           "cb_cache_fork_workspace_bytes", "cb_cache_fork", "cb_cache_compact_workspace_bytes",
+           "cb_cache_compact", "cb_cache_write", "cb_cache_read",
+           "cb_cache_attend_workspace_bytes", "cb_cache_attend",
            "Buffers", "run_steps", "run_pipeline", "CB_F32", "CB_BF16",
            "LIB_PATH"]

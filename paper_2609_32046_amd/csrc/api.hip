@@ -504,6 +504,7 @@ const char* cb_status_string(int status) {
     case CB_ERR_ALIGN: return "device pointer not 16-byte aligned";
     case CB_ERR_HIP: return "HIP launch error";
     case CB_ERR_TIMEOUT: return "a dependency wait in the score kernel timed out";
+    case CB_ERR_PAGES: return "too few free pages in the cache";
     default: return "unknown status";
   }
 }

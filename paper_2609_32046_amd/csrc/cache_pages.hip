@@ -1,0 +1,561 @@
+// Pages of the four-bit cache (gfx950): taking, sharing, copying, thinning and
+// giving back.
+//
+// The free list is the reference counts themselves: a page of no holder is
+// free, and the lowest free ones are taken first.  So there is one state to keep
+// right, and every call's outcome is a function of it.  A call that takes pages
+// plans in one workgroup (it checks every entry before it changes anything,
+// and takes back what it released when pages lack), then moves bytes with the
+// whole device.
+#include "cache.h"
+
+namespace cb {
+namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kPlan = 1024;         // threads of a planning workgroup
+constexpr int kPlanWaves = kPlan / 64;
+constexpr int kScan = 4;            // 16-byte reads of refs a thread has under way
+
+__device__ inline int held_pages(const CacheView& c, int len) {
+  const int64_t n = ((int64_t)(len > 0 ? len : 0) + (1 << c.page_shift) - 1) >> c.page_shift;
+  return n < c.width ? (int)n : c.width;
+}
+
+__device__ inline bool known(const CacheView& c, int seq) {
+  return (unsigned)seq < (unsigned)c.seqs;
+}
+
+__device__ inline int wave_sum(int x) {
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) x += __shfl_xor(x, d);
+  return x;
+}
+
+// Inclusive sum over the lanes up to this one.
+__device__ inline int wave_scan(int x) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int y = __shfl_up(x, d);
+    if (lane >= d) x += y;
+  }
+  return x;
+}
+
+// Exclusive prefix of x over the workgroup, and the total.  `sums`: kPlanWaves
+// words; two barriers.
+__device__ inline int group_scan(int x, int* sums, int* total) {
+  const int wave = threadIdx.x >> 6;
+  const int incl = wave_scan(x);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 63) sums[wave] = incl;
+  __syncthreads();
+  int before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < kPlanWaves; ++w) {
+    const int v = sums[w];
+    before += w < wave ? v : 0;
+    all += v;
+  }
+  *total = all;
+  return before + incl - x;
+}
+
+// Bit set of sequences in LDS; true when the bit was set before.
+__device__ inline bool mark(uint32_t* bits, int seq) {
+  const uint32_t b = 1u << (seq & 31);
+  return (atomicOr(&bits[seq >> 5], b) & b) != 0;
+}
+__device__ inline bool marked(const uint32_t* bits, int seq) {
+  return (bits[seq >> 5] >> (seq & 31)) & 1u;
+}
+
+struct PlanShared {
+  int sums[kPlanWaves];
+  int bad;
+  int found;
+  int offset[kCacheMaxEntries + 1];   // pages that the entries before need
+};
+
+// Gives a page back; a count that was zero (a page listed by mistake) stays.
+__device__ inline void drop(int32_t* refs, int page) {
+  if (atomicSub(&refs[page], 1) <= 0) atomicAdd(&refs[page], 1);
+}
+
+// Offsets of the entries' needs, need(i) pages each; returns the total.
+template <typename Need>
+__device__ inline int64_t plan_offsets(PlanShared& sh, int n, Need need) {
+  int64_t base = 0;
+  for (int i0 = 0; i0 < n; i0 += kPlan) {
+    const int i = i0 + threadIdx.x;
+    int total;
+    const int before = group_scan(i < n ? need(i) : 0, sh.sums, &total);
+    const int64_t at = base + before;
+    if (i < n) sh.offset[i] = at > kCacheMaxPages ? kCacheMaxPages + 1 : (int)at;
+    base += total;
+  }
+  if (threadIdx.x == 0) sh.offset[n] = base > kCacheMaxPages ? kCacheMaxPages + 1 : (int)base;
+  __syncthreads();
+  return base;
+}
+
+// Calls take(page, rank) for the free pages of lowest number, ranks 0..want-1
+// in order of their numbers, and returns how many there are (at most want).  refs are read
+// with device scope: this workgroup's own atomics have changed them.
+template <typename Take>
+__device__ inline int64_t scan_free(const CacheView& c, PlanShared& sh, int64_t want, Take take) {
+  int64_t base = 0;
+  constexpr int kStep = kPlan * 4 * kScan;
+  for (int64_t p0 = 0; p0 < c.pages && base < want; p0 += kStep) {
+    // thread i holds pages p0 + (j * kPlan + i) * 4 ..: every j a contiguous piece
+    i32x4 r[kScan];
+#pragma unroll
+    for (int j = 0; j < kScan; ++j) {
+      const int64_t p = p0 + ((int64_t)j * kPlan + threadIdx.x) * 4;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        r[j][e] = p + e < c.pages ? __hip_atomic_load(&c.refs[p + e], __ATOMIC_RELAXED,
+                                                       __HIP_MEMORY_SCOPE_AGENT)
+                                  : 1;
+    }
+#pragma unroll
+    for (int j = 0; j < kScan; ++j) {
+      int mine = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) mine += r[j][e] == 0;
+      int total;
+      int64_t rank = base + group_scan(mine, sh.sums, &total);
+      const int64_t p = p0 + ((int64_t)j * kPlan + threadIdx.x) * 4;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (r[j][e] == 0) {
+          if (rank < want) take((int)(p + e), (int)rank);
+          ++rank;
+        }
+      base += total;
+      if (base >= want) break;   // the same in every thread
+    }
+  }
+  return base < want ? base : want;
+}
+
+// Entry whose pages include rank r.
+__device__ inline int entry_of(const PlanShared& sh, int n, int r) {
+  int lo = 0, hi = n - 1;   // offset[lo] <= r < offset[hi + 1]
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (sh.offset[mid] <= r) lo = mid;
+    else hi = mid - 1;
+  }
+  return lo;
+}
+
+__device__ inline void clear_bits(uint32_t* bits, int seqs) {
+  for (int i = threadIdx.x; i < (seqs + 31) / 32; i += kPlan) bits[i] = 0u;
+}
+
+// ---------------------------------------------------------------------------
+
+__global__ __launch_bounds__(kPlan) void cache_extend_kernel(CacheView c,
+                                                             const int32_t* __restrict__ seqs,
+                                                             const int32_t* __restrict__ add,
+                                                             int n, int32_t* status) {
+  extern __shared__ uint32_t bits[];
+  __shared__ PlanShared sh;
+  clear_bits(bits, c.seqs);
+  if (threadIdx.x == 0) sh.bad = 0;
+  __syncthreads();
+  const int64_t room = (int64_t)c.width << c.page_shift;
+  for (int i = threadIdx.x; i < n; i += kPlan) {
+    const int s = seqs[i];
+    if (!known(c, s) || mark(bits, s) || add[i] < 0 || c.lens[s] < 0 ||
+        (int64_t)c.lens[s] + add[i] > room)
+      sh.bad = 1;
+  }
+  __syncthreads();
+  if (sh.bad) {
+    if (threadIdx.x == 0) *status = -1;
+    return;
+  }
+  const int64_t want = plan_offsets(sh, n, [&](int i) {
+    const int len = c.lens[seqs[i]];
+    return held_pages(c, len + add[i]) - held_pages(c, len);
+  });
+  const int64_t have = scan_free(c, sh, want, [](int, int) {});
+  if (have < want) {
+    if (threadIdx.x == 0) *status = (int)(want - have < 0x7fffffff ? want - have : 0x7fffffff);
+    return;
+  }
+  scan_free(c, sh, want, [&](int page, int rank) {
+    const int i = entry_of(sh, n, rank);
+    const int s = seqs[i];
+    c.table[(int64_t)s * c.width + held_pages(c, c.lens[s]) + rank - sh.offset[i]] = page;
+    c.refs[page] = 1;
+  });
+  __syncthreads();   // lens are read above
+  for (int i = threadIdx.x; i < n; i += kPlan) c.lens[seqs[i]] += add[i];
+  if (threadIdx.x == 0) *status = 0;
+}
+
+__global__ __launch_bounds__(256) void cache_free_kernel(CacheView c,
+                                                         const int32_t* __restrict__ seqs) {
+  const int s = seqs[blockIdx.x];
+  if (!known(c, s)) return;
+  __shared__ int len;
+  if (threadIdx.x == 0) len = atomicExch(&c.lens[s], 0);   // an entry listed again finds 0
+  __syncthreads();
+  const int pages = held_pages(c, len);
+  int32_t* row = c.table + (int64_t)s * c.width;
+  for (int j = threadIdx.x; j < pages; j += 256) {
+    const int p = row[j];
+    row[j] = -1;
+    if ((unsigned)p < (unsigned)c.pages) drop(c.refs, p);
+  }
+}
+
+// Adds d to the holders of every page of the listed sequences (release: -1,
+// taking back: +1).  Rows of table, one wave each.
+__device__ inline void add_refs(const CacheView& c, const int32_t* seqs, int n, int d,
+                                const int32_t* unless) {
+  const int lane = threadIdx.x & 63;
+  for (int i = threadIdx.x >> 6; i < n; i += kPlanWaves) {
+    const int s = seqs[i];
+    if (unless && unless[i] == s) continue;
+    const int pages = held_pages(c, c.lens[s]);
+    for (int j = lane; j < pages; j += 64) {
+      const int p = c.table[(int64_t)s * c.width + j];
+      if ((unsigned)p < (unsigned)c.pages) atomicAdd(&c.refs[p], d);
+    }
+  }
+}
+
+// ws of a fork: how many pages are copied (padded to 16 bytes), then (from, to).
+__global__ __launch_bounds__(kPlan) void cache_fork_kernel(CacheView c,
+                                                           const int32_t* __restrict__ parents,
+                                                           const int32_t* __restrict__ children,
+                                                           int n, int copy, int32_t* status,
+                                                           int32_t* count, int2* pairs) {
+  extern __shared__ uint32_t bits[];
+  __shared__ PlanShared sh;
+  const int lane = threadIdx.x & 63;
+  clear_bits(bits, c.seqs);
+  if (threadIdx.x == 0) {
+    sh.bad = 0;
+    *count = 0;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += kPlan)
+    if (!known(c, parents[i]) || !known(c, children[i]) || mark(bits, children[i])) sh.bad = 1;
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += kPlan)
+    if (known(c, parents[i]) && marked(bits, parents[i])) sh.bad = 1;
+  __syncthreads();
+  if (!sh.bad)   // every page that a parent says it holds is one
+    for (int i = threadIdx.x >> 6; i < n; i += kPlanWaves) {
+      const int s = parents[i], pages = held_pages(c, c.lens[s]);
+      for (int j = lane; j < pages; j += 64)
+        if ((unsigned)c.table[(int64_t)s * c.width + j] >= (unsigned)c.pages) sh.bad = 1;
+    }
+  __syncthreads();
+  if (sh.bad) {
+    if (threadIdx.x == 0) *status = -1;
+    return;
+  }
+  add_refs(c, children, n, -1, nullptr);
+  const int part = (1 << c.page_shift) - 1;
+  const int64_t want = plan_offsets(sh, n, [&](int i) {
+    const int len = c.lens[parents[i]];
+    return copy ? held_pages(c, len) : (len > 0 && (len & part) != 0);
+  });
+  __threadfence();
+  __syncthreads();
+  const int64_t have = scan_free(c, sh, want, [](int, int) {});
+  if (have < want) {
+    add_refs(c, children, n, 1, nullptr);
+    if (threadIdx.x == 0) *status = (int)(want - have < 0x7fffffff ? want - have : 0x7fffffff);
+    return;
+  }
+  // which pages are copied, and where to; the children's own rows follow
+  scan_free(c, sh, want, [&](int page, int rank) {
+    const int i = entry_of(sh, n, rank);
+    const int s = parents[i];
+    const int j = copy ? rank - sh.offset[i] : held_pages(c, c.lens[s]) - 1;
+    pairs[rank] = make_int2(c.table[(int64_t)s * c.width + j], page);
+    c.refs[page] = 1;
+  });
+  __threadfence_block();
+  __syncthreads();
+  for (int i = threadIdx.x >> 6; i < n; i += kPlanWaves) {
+    const int s = parents[i], d = children[i];
+    const int len = c.lens[s], pages = held_pages(c, len), before = held_pages(c, c.lens[d]);
+    const int own = sh.offset[i + 1] - sh.offset[i];
+    for (int j = lane; j < pages; j += 64) {
+      int p;
+      if (j >= pages - own) {
+        p = pairs[sh.offset[i] + j - (pages - own)].y;
+      } else {
+        p = c.table[(int64_t)s * c.width + j];
+        atomicAdd(&c.refs[p], 1);
+      }
+      c.table[(int64_t)d * c.width + j] = p;
+    }
+    for (int j = pages + lane; j < before; j += 64) c.table[(int64_t)d * c.width + j] = -1;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += kPlan) c.lens[children[i]] = c.lens[parents[i]];
+  if (threadIdx.x == 0) {
+    *status = 0;
+    *count = (int)want;
+  }
+}
+
+// Whole pages, 16 bytes a lane, four of them under way.
+__global__ __launch_bounds__(256) void cache_copy_kernel(unsigned char* pool, int64_t page_bytes,
+                                                         const int32_t* __restrict__ count,
+                                                         const int2* __restrict__ pairs,
+                                                         int pieces) {
+  constexpr int kVec = 4, kPiece = 256 * kVec;
+  const int n = *count;
+  const int64_t vecs = page_bytes / 16;
+  const int64_t items = (int64_t)n * pieces;
+  for (int64_t w = blockIdx.x; w < items; w += gridDim.x) {
+    const int e = (int)(w / pieces);
+    const int64_t v0 = (w - (int64_t)e * pieces) * kPiece + threadIdx.x;
+    const int2 pr = pairs[e];
+    const u32x4* from = reinterpret_cast<const u32x4*>(pool + pr.x * page_bytes);
+    u32x4* to = reinterpret_cast<u32x4*>(pool + pr.y * page_bytes);
+    u32x4 x[kVec];
+#pragma unroll
+    for (int j = 0; j < kVec; ++j)
+      if (v0 + j * 256 < vecs) x[j] = from[v0 + j * 256];
+#pragma unroll
+    for (int j = 0; j < kVec; ++j)
+      if (v0 + j * 256 < vecs) to[v0 + j * 256] = x[j];
+  }
+}
+
+// ---------------------------------------------------------------------------
+// compaction
+
+__device__ inline int64_t kept(const CacheCompactArgs& a, int i) {
+  return a.counts ? (int64_t)a.counts[i] : a.keep;
+}
+
+// The plan: dst's pages, and the sources' rows as they were, for the gather
+// that follows (dst may be src).
+__global__ __launch_bounds__(kPlan) void cache_compact_plan_kernel(CacheCompactArgs a) {
+  extern __shared__ uint32_t bits[];
+  __shared__ PlanShared sh;
+  const CacheView& c = a.c;
+  const int lane = threadIdx.x & 63, n = a.n;
+  clear_bits(bits, c.seqs);
+  if (threadIdx.x == 0) sh.bad = 0;
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += kPlan) {
+    const int64_t k = kept(a, i);
+    if (!known(c, a.src[i]) || !known(c, a.dst[i]) || k < 0 || k > a.keep ||
+        mark(bits, a.dst[i]))
+      sh.bad = 1;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += kPlan)
+    if (known(c, a.src[i]) && marked(bits, a.src[i]) && a.dst[i] != a.src[i]) sh.bad = 1;
+  __syncthreads();
+  if (sh.bad) {
+    if (threadIdx.x == 0) *a.status = -1;
+    return;
+  }
+  add_refs(c, a.dst, n, -1, a.src);   // not those that are read
+  const int64_t P = 1 << c.page_shift;
+  const int64_t want =
+      plan_offsets(sh, n, [&](int i) { return (int)((kept(a, i) + P - 1) >> c.page_shift); });
+  __threadfence();
+  __syncthreads();
+  const int64_t have = scan_free(c, sh, want, [](int, int) {});
+  if (have < want) {
+    add_refs(c, a.dst, n, 1, a.src);
+    if (threadIdx.x == 0) *a.status = (int)(want - have < 0x7fffffff ? want - have : 0x7fffffff);
+    return;
+  }
+  for (int i = threadIdx.x >> 6; i < n; i += kPlanWaves) {
+    const int s = a.src[i], len = c.lens[s], pages = held_pages(c, len);
+    int32_t* old = a.old_rows + (int64_t)i * (c.width + 1);
+    if (lane == 0) old[0] = len;
+    for (int j = lane; j < pages; j += 64) old[1 + j] = c.table[(int64_t)s * c.width + j];
+  }
+  __threadfence_block();
+  __syncthreads();
+  scan_free(c, sh, want, [&](int page, int rank) {
+    const int i = entry_of(sh, n, rank);
+    c.table[(int64_t)a.dst[i] * c.width + rank - sh.offset[i]] = page;
+    c.refs[page] = 1;
+  });
+  __threadfence();
+  __syncthreads();
+  for (int i = threadIdx.x >> 6; i < n; i += kPlanWaves) {
+    const int d = a.dst[i], before = held_pages(c, c.lens[d]);
+    const int32_t* old = a.old_rows + (int64_t)i * (c.width + 1);
+    for (int j = sh.offset[i + 1] - sh.offset[i] + lane; j < before; j += 64)
+      c.table[(int64_t)d * c.width + j] = -1;
+    if (a.src[i] == d)   // its old pages, which the gather still reads
+      for (int j = lane; j < before; j += 64)
+        if ((unsigned)old[1 + j] < (unsigned)c.pages) drop(c.refs, old[1 + j]);
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += kPlan) c.lens[a.dst[i]] = (int)kept(a, i);
+  if (threadIdx.x == 0) *a.status = 0;
+}
+
+// 16 new positions of one unit a wave: 16 rows of key codes by four (D = 128) or
+// two (64) lanes of 16 bytes; four lanes' blocks of value codes, each lane's 16 (8)
+// bytes from the four positions' own places.
+template <int D>
+__global__ __launch_bounds__(256) void cache_gather_kernel(CacheCompactArgs a, int blocks_per_unit,
+                                                           int64_t items) {
+  if (*a.status != 0) return;   // the plan changed nothing
+  const CacheView& c = a.c;
+  const int P = 1 << c.page_shift;
+  const int lane = threadIdx.x & 63;
+  const int units = c.layers * c.heads;
+  constexpr int G = D / 32;
+  const int64_t waves = (int64_t)gridDim.x * 4;
+  for (int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); w < items; w += waves) {
+    const int64_t eb = w / units;
+    const int u = (int)(w - eb * units);
+    const int i = (int)(eb / blocks_per_unit);
+    const int64_t j0 = (eb - (int64_t)i * blocks_per_unit) * 16;
+    const int64_t cnt = kept(a, i);
+    if (j0 >= ((cnt + P - 1) & ~(int64_t)(P - 1))) continue;
+    const int layer = u / c.heads, head = u - layer * c.heads;
+    const int32_t* old = a.old_rows + (int64_t)i * (c.width + 1);
+    const int32_t* idx = a.idx + i * a.idx_stride[0] + layer * a.idx_stride[1] +
+                         head * a.idx_stride[2];
+    const int page = c.table[(int64_t)a.dst[i] * c.width + (j0 >> c.page_shift)];
+    const int64_t unit_off = (int64_t)u * c.unit_bytes;
+    unsigned char* to = c.pool + page * c.page_bytes + unit_off;
+    const int at0 = (int)(j0 & (P - 1));
+    // lane l (of 16) holds the source of new position j0 + l: its unit and place
+    const int len = old[0];
+    const int l16 = lane & 15;
+    int at = -1, spage = 0;
+    if (j0 + l16 < cnt) {
+      const int s = idx[j0 + l16];
+      if (s >= 0 && s < len && (s >> c.page_shift) < c.width) {
+        const int p = old[1 + (s >> c.page_shift)];
+        if ((unsigned)p < (unsigned)c.pages) {
+          spage = p;
+          at = s & (P - 1);
+        }
+      }
+    }
+    // keys
+    constexpr int kRowLanes = D / 32;   // lanes of 16 bytes a row of codes
+    if (lane < 16 * kRowLanes) {
+      const int row = lane / kRowLanes, b = lane % kRowLanes;
+      const int p = __shfl(spage, row), t = __shfl(at, row);
+      u32x4 x = {0u, 0u, 0u, 0u};
+      if (t >= 0)
+        x = *reinterpret_cast<const u32x4*>(c.pool + p * c.page_bytes + unit_off + t * (D / 2) +
+                                            b * 16);
+      *reinterpret_cast<u32x4*>(to + (at0 + row) * (D / 2) + b * 16) = x;
+    }
+    // values: lane (block = lane / 16, run = lane % 16)
+    const int blk = lane >> 4, run = lane & 15;
+    const unsigned char* vfrom[4];
+    int vt[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int p = __shfl(spage, blk * 4 + e);
+      vt[e] = __shfl(at, blk * 4 + e);
+      vfrom[e] = c.pool + p * c.page_bytes + unit_off + unit_value_codes(P, D) +
+                 (vt[e] >> 2) * (2 * D) + run * (D / 8) + (vt[e] & 3) * (D / 32);
+    }
+    unsigned char* vto = to + unit_value_codes(P, D) + ((at0 >> 2) + blk) * (2 * D) + run * (D / 8);
+    if constexpr (D == 128) {
+      u32x4 x;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        x[e] = vt[e] >= 0 ? *reinterpret_cast<const uint32_t*>(vfrom[e]) : 0u;
+      *reinterpret_cast<u32x4*>(vto) = x;
+    } else {
+      uint32_t h[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        h[e] = vt[e] >= 0 ? *reinterpret_cast<const uint16_t*>(vfrom[e]) : 0u;
+      *reinterpret_cast<uint2*>(vto) = make_uint2(h[0] | (h[1] << 16), h[2] | (h[3] << 16));
+    }
+    // scales: lane = (position, group); rows without a source get the least
+    if (lane < 16 * G) {
+      const int row = lane / G, g = lane % G;
+      const int p = __shfl(spage, row), t = __shfl(at, row);
+      unsigned char ks = 3, vs = 3;
+      if (t >= 0) {
+        const unsigned char* from = c.pool + p * c.page_bytes + unit_off;
+        ks = from[unit_key_scales(P, D) + t * G + g];
+        vs = from[unit_value_scales(P, D) + ((t >> 2) * G + g) * 4 + (t & 3)];
+      }
+      const int q = at0 + row;
+      to[unit_key_scales(P, D) + q * G + g] = ks;
+      to[unit_value_scales(P, D) + ((q >> 2) * G + g) * 4 + (q & 3)] = vs;
+    }
+  }
+}
+
+size_t bit_bytes(const CacheView& c) { return (size_t)((c.seqs + 31) / 32) * sizeof(uint32_t); }
+
+}  // namespace
+
+hipError_t launch_cache_extend(const CacheView& c, const int32_t* seqs, const int32_t* add, int n,
+                               int32_t* status, hipStream_t s) {
+  cache_extend_kernel<<<1, kPlan, bit_bytes(c), s>>>(c, seqs, add, n, status);
+  return hipGetLastError();
+}
+
+hipError_t launch_cache_free(const CacheView& c, const int32_t* seqs, int n, hipStream_t s) {
+  if (n == 0) return hipSuccess;
+  cache_free_kernel<<<(unsigned)n, 256, 0, s>>>(c, seqs);
+  return hipGetLastError();
+}
+
+size_t cache_fork_ws(int64_t n, int64_t width) {
+  return 16 + (((size_t)n * (size_t)width * sizeof(int2) + 15) & ~(size_t)15);
+}
+
+hipError_t launch_cache_fork(const CacheView& c, const int32_t* parents, const int32_t* children,
+                             int n, bool copy, int32_t* status, void* ws, hipStream_t s) {
+  int32_t* count = static_cast<int32_t*>(ws);
+  int2* pairs = reinterpret_cast<int2*>(static_cast<unsigned char*>(ws) + 16);
+  cache_fork_kernel<<<1, kPlan, bit_bytes(c), s>>>(c, parents, children, n, copy ? 1 : 0, status,
+                                                   count, pairs);
+  if (n > 0) {
+    const int64_t vecs = c.page_bytes / 16;
+    const int pieces = (int)((vecs + 1023) / 1024);
+    const int64_t most = (int64_t)n * (copy ? c.width : 1) * pieces;
+    const unsigned grid = (unsigned)(most < 4096 ? most : 4096);
+    cache_copy_kernel<<<grid, 256, 0, s>>>(c.pool, c.page_bytes, count, pairs, pieces);
+  }
+  return hipGetLastError();
+}
+
+size_t cache_compact_ws(int64_t n, int64_t width) {
+  return ((size_t)n * (size_t)(width + 1) * sizeof(int32_t) + 15) & ~(size_t)15;
+}
+
+hipError_t launch_cache_compact(const CacheCompactArgs& a, hipStream_t s) {
+  cache_compact_plan_kernel<<<1, kPlan, bit_bytes(a.c), s>>>(a);
+  if (a.n > 0) {
+    const int64_t P = 1 << a.c.page_shift;
+    const int blocks = (int)((a.keep + P - 1) / P * (P / 16));
+    const int64_t items = (int64_t)a.n * blocks * a.c.layers * a.c.heads;
+    const int64_t groups = (items + 3) / 4;
+    const unsigned grid = (unsigned)(groups < 4096 ? groups : 4096);
+    if (a.c.D == 64) cache_gather_kernel<64><<<grid, 256, 0, s>>>(a, blocks, items);
+    else cache_gather_kernel<128><<<grid, 256, 0, s>>>(a, blocks, items);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace cb
