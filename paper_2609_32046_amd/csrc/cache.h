@@ -93,13 +93,13 @@ struct AttendArgs {
   float* lse;
   const int32_t* seqs;
   const int32_t* q_lens;
-  float* part_o;    // [layers][heads][slots][rows_pad][D]
+  float* part_o;    // [layers][heads][slots][rows_pad][D], slot = run + sequence
   float2* part_ml;  // [layers][heads][slots][rows_pad]: reference, sum
   int64_t q_stride[4], out_stride[4];
   int64_t q_len;    // m
   int32_t layer0, layers, n, q_heads, group;
   int32_t row_tiles, rows_pad;
-  int32_t target;   // chunks a (layer, head, row tile) is split into, about
+  int32_t target;   // runs that the positions are dealt to
   int32_t slots;    // target + n
   int32_t causal;
   float c2;         // scale * log2(e)

@@ -384,7 +384,8 @@ int cb_cache_attend(const cb_cache* c, int32_t layer0, int32_t layers, const int
   a.slots = p.slots;
   a.causal = causal != 0;
   const double sc = scale == 0.0 ? 1.0 / sqrt((double)c->head_dim) : scale;
-  a.c2 = (float)(sc * 1.4426950408889634);
+  // never 0: a masked logit is -inf times it
+  a.c2 = fmaxf((float)(sc * 1.4426950408889634), 1e-37f);
   return done(cb::launch_cache_attend(a, p, dtype == CB_F32, static_cast<hipStream_t>(stream)));
 }
 

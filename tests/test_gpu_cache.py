@@ -487,6 +487,12 @@ def fill_cache(torch, cb, c, lens, seed, layers=1, start=None):
     cb.cb_cache_write(c.desc, k.cuda(), v.cuda(), start=ints(torch, [0] * n), counts=ints(torch, lens))
 
 
+def scratch(torch, cb, c, q):
+    """Scratch of an attention call, of any contents."""
+    n = cb.cb_cache_attend_workspace_bytes(c.desc, q.shape[0], q.shape[1], q.shape[2], q.shape[3])
+    return torch.randint(0, 256, (n,), dtype=torch.uint8, device="cuda") if n else None
+
+
 def attend_case(torch, cb, lens, Hkv, G, D, P, m, dtype, causal, seqs=None, q_lens=None, layers=1, layer0=0,
                 scale=0.0, seed=0, holes=(), prepare=None, extra=3):
     c = cache_with(torch, cb, lens, L=layers + layer0, H=Hkv, D=D, P=P, seed=seed, extra=extra)
@@ -500,8 +506,7 @@ def attend_case(torch, cb, lens, Hkv, G, D, P, m, dtype, causal, seqs=None, q_le
     q = randn(torch, seed + 5, layers, n, Hkv * G, m, D).to(dt(torch, dtype)).cuda()
     out = torch.full_like(q, 7.0)
     lse = torch.full(q.shape[:4], 7.0, device="cuda")
-    nb = cb.cb_cache_attend_workspace_bytes(c.desc, layers, n, Hkv * G, m)
-    ws = torch.randint(0, 256, (nb,), dtype=torch.uint8, device="cuda") if nb else None
+    ws = scratch(torch, cb, c, q)
     cb.cb_cache_attend(c.desc, q, out, ws, lse, None if seqs is None else ints(torch, seqs),
                        None if q_lens is None else ints(torch, q_lens), causal, scale, layer0)
     clipped = [m] * n if q_lens is None else [max(0, min(x, m)) for x in q_lens]
@@ -604,7 +609,7 @@ def test_attend_positions_without_a_page(torch, cb):
     c.table[0, 1] = c.pool.shape[0] + 5
     q = randn(torch, 1, 1, 3, 2, 1, 64).cuda()
     out, lse = torch.ones_like(q), torch.ones(q.shape[:4], device="cuda")
-    cb.cb_cache_attend(c.desc, q, out, None, lse, seqs=ints(torch, [0, 99, -1]))
+    cb.cb_cache_attend(c.desc, q, out, scratch(torch, cb, c, q), lse, seqs=ints(torch, [0, 99, -1]))
     assert not out[:, 1:].any() and (lse[:, 1:] == -math.inf).all()
     m = model(c, 64, 16)
     check_attend(torch, m, q[:, :1], out[:, :1], lse[:, :1], [0], [1], True, 0.0, 0, "f32")
@@ -619,7 +624,7 @@ def test_attend_strided_rows(torch, cb):
     q = buf[:, :, :Hkv * G].transpose(1, 2)[None]
     room = torch.full((2, m, Hkv * G + 1, D), 7.0, dtype=torch.bfloat16, device="cuda")
     out = room[:, :, 1:].transpose(1, 2)[None]
-    cb.cb_cache_attend(c.desc, q, out)
+    cb.cb_cache_attend(c.desc, q, out, scratch(torch, cb, c, q))
     check_attend(torch, model(c, D, P), q, out, None, [0, 1], [m, m], True, 0.0, 0, "bf16")
     assert (room[:, :, 0] == 7.0).all()
 
