@@ -289,9 +289,11 @@ __global__ __launch_bounds__(kThreads, RT == 1 && !F32 ? 3 : 2) void attend_kern
   constexpr int VT = D / 16;              // second: tiles of 16 values
   constexpr int NQ = F32 ? 3 : 1;
   constexpr int NB = RT == 1 && !F32 ? 3 : 2;     // steps of codes in registers, all but one under way
+  constexpr bool kSharedQ = !F32 && RT > 1;       // the four waves' query rows are the same
   constexpr int kPad = 4;
   __shared__ float so[kWaves][16][D + kPad];
   __shared__ float sm[kWaves][RT * 16], sl[kWaves][RT * 16];
+  __shared__ bf16x8 sq[kSharedQ ? RT : 1][KS][kSharedQ ? 64 : 1];
 
   const int lane = threadIdx.x & 63;
   const int wave = uniform((int)threadIdx.x >> 6);
@@ -355,9 +357,21 @@ __global__ __launch_bounds__(kThreads, RT == 1 && !F32 ? 3 : 2) void attend_kern
     const int hi = see_last < end ? (see_last > 0 ? see_last : 0) : end;
 
     // before the codes, whose loads the loop keeps under way
-    Query<D, F32> q[RT];
+    Query<D, F32> q[kSharedQ ? 1 : RT];
 #pragma unroll
-    for (int t = 0; t < RT; ++t) q[t].load(qp[t], g, live[t]);
+    for (int t = 0; t < RT; ++t) {
+      if constexpr (kSharedQ) {
+        // held in LDS, in the lanes' order: 16 reads a step of 64 rows, against 64 registers
+        if ((t & (kWaves - 1)) == wave) {
+          q[0].load(qp[t], g, live[t]);
+#pragma unroll
+          for (int j = 0; j < KS; ++j) sq[t][j][lane] = q[0].x[j][0];
+        }
+      } else {
+        q[t].load(qp[t], g, live[t]);
+      }
+    }
+    if (kSharedQ) __syncthreads();
 
     const int steps = hi <= lo ? 0 : (hi - lo + kRound - 1) / kRound;
     // The page table through the scalar cache: its waits are apart from those for the codes,
@@ -440,7 +454,8 @@ __global__ __launch_bounds__(kThreads, RT == 1 && !F32 ? 3 : 2) void attend_kern
             for (int u = NQ - 1; u >= 0; --u)   // small parts first
 #pragma unroll
               for (int j = 0; j < KS; ++j)
-                s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk[h][j], q[t].x[j][u], s[h], 0, 0, 0);
+                s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                    kk[h][j], kSharedQ ? sq[t][j][lane] : q[kSharedQ ? 0 : t].x[j][u], s[h], 0, 0, 0);
           }
           if (masked) {
 #pragma unroll
@@ -704,10 +719,12 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, uint32_t
 
 template <int D, bool F32>
 hipError_t launch(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
+  constexpr int kMost = !F32 ? 4 : D == 64 ? 2 : 1;   // blocks of a wave, as in make_attend_plan
   const int64_t grid = (int64_t)a.c.heads * a.row_tiles * a.target * a.layers;
   if (grid > 0x7fffffff) return hipErrorInvalidValue;
   if (p.blocks == 1) attend_kernel<D, F32, 1><<<(unsigned)grid, kThreads, 0, s>>>(a);
-  else attend_kernel<D, F32, 2><<<(unsigned)grid, kThreads, 0, s>>>(a);
+  else if (F32 || p.blocks == 2) attend_kernel<D, F32, kMost < 2 ? kMost : 2><<<(unsigned)grid, kThreads, 0, s>>>(a);
+  else attend_kernel<D, F32, kMost><<<(unsigned)grid, kThreads, 0, s>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.total == 0) return e;   // one run: nothing to join
   const int64_t rows = a.q_len * a.group;
@@ -722,22 +739,36 @@ hipError_t launch(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
 // Workgroups resident at a time: 256 compute units, three each of the
 // 16-row kernels, two of the others.
 constexpr int64_t kUnits = 256;
+// Rounds of the shortest run: joining costs a launch, about as long as eight rounds take.
+constexpr int64_t kShortest = 4;
 
 bool make_attend_plan(int layers, int n, int heads, int q_heads, int64_t q_len, int D, bool f32,
                       int64_t capacity, AttendPlan* p) {
   const int64_t rows = q_len * (q_heads / heads);
   if (rows > (1 << 26)) return false;
-  // two blocks share a step's conversions; with fp32 rows of 128 they do not fit the
-  // registers (72 spills)
-  p->blocks = rows <= 16 || (f32 && D == 128) ? 1 : 2;
+  // blocks of a wave share a step's conversions; with fp32 rows two do not fit the
+  // registers at D = 128
+  p->blocks = rows <= 16 || (f32 && D == 128) ? 1 : rows <= 32 || f32 ? 2 : 4;
   const int64_t per = p->blocks * 16;
   const int64_t tiles = (rows + per - 1) / per;
   const int64_t sets = tiles * heads * layers;
   const int64_t resident = kUnits * (p->blocks == 1 ? 3 : 2);
-  int64_t target = resident / sets;
-  // no run shorter than two rounds even where every sequence is full
-  const int64_t most = (int64_t)n * ((capacity + 2 * kRound - 1) / (2 * kRound));
-  target = target < 1 ? 1 : target > most ? most : target;
+  // no run shorter than kShortest rounds even where every sequence is full
+  const int64_t most = (int64_t)n * ((capacity + kShortest * kRound - 1) / (kShortest * kRound));
+  // Workgroups run in rounds of `resident`: the number of runs that leaves least of the last
+  // one idle, the pieces of a further run counting for a fiftieth.
+  int64_t target = 1;
+  double best = 0.0;
+  const int64_t first = resident / sets > 1 ? resident / sets : 1;
+  for (int64_t t = first; t <= first + 7; ++t) {
+    const int64_t turns = (sets * t + resident - 1) / resident;
+    const double used = (double)(sets * t) / (double)(turns * resident) - 0.02 * (double)(t - first);
+    if (used > best) {
+      best = used;
+      target = t;
+    }
+  }
+  if (target > most) target = most;
   p->row_tiles = (int32_t)tiles;
   p->rows_pad = (int32_t)(tiles * per);
   p->target = (int32_t)target;
