@@ -401,50 +401,63 @@ class PositionBuffers:
 # The receiver's side: rotary positions, the paged four-bit cache, attention
 
 
-def _tensor(x, where, dtypes=None, ndim=None, shape=None):
-    """Checks of a tensor argument that its pointer cannot show: type, shape
-    (None: any size), and that it lies on the current device."""
-    import torch
-
-    if x.device.type != "cuda" or x.device.index != torch.cuda.current_device():
-        raise CBError(-2, f"{where}: tensor on {x.device}, not on the current device")
-    if dtypes is not None and x.dtype not in dtypes:
-        raise CBError(-3, f"{where}: {x.dtype}")
-    if ndim is not None and x.dim() != ndim:
-        raise CBError(-2, f"{where}: {x.dim()} axes, {ndim} wanted")
-    if shape is not None and (x.dim() != len(shape) or any(
-            s is not None and s != n for n, s in zip(x.shape, shape))):
-        raise CBError(-2, f"{where}: shape {tuple(x.shape)}, {tuple(shape)} wanted")
-    return x
+_S3, _S4 = _i64 * 3, _i64 * 4
+_byref = ctypes.byref
+_torch = None
 
 
-def _ints(x, where, n=None):
-    """A contiguous int32 list (of n entries), or None."""
-    import torch
+def _lazy_torch():
+    global _torch
+    if _torch is None:
+        import torch
 
+        _torch = torch
+    return _torch
+
+
+def _now(stream):
+    """(current device, stream as an integer): looked up once a call, as these calls take some
+    microseconds in all."""
+    torch = _torch or _lazy_torch()
+    dev = torch.cuda.current_device()
+    if stream is None:
+        return dev, torch.cuda.current_stream(dev).cuda_stream
+    return dev, stream if isinstance(stream, int) else stream.cuda_stream
+
+
+def _refuse(where, x, what, status=-2):
+    raise CBError(status, f"{where}: {what} (got {tuple(x.shape)} {x.dtype} on {x.device})")
+
+
+def _ints(x, where, dev, n=None):
+    """Address of a contiguous int32 list (of n entries) on the current device; None for None."""
     if x is None:
         return None
-    _tensor(x, where, (torch.int32,), 1, None if n is None else (n,))
-    if not x.is_contiguous():
-        raise CBError(-2, f"{where}: not contiguous")
-    return x
+    if x.dtype is not _torch.int32:
+        _refuse(where, x, "an int32 list is wanted", -3)
+    if x.dim() != 1 or (n is not None and x.shape[0] != n) or not x.is_contiguous():
+        _refuse(where, x, f"a contiguous list of {'any' if n is None else n} entries is wanted")
+    if x.get_device() != dev:
+        _refuse(where, x, "not on the current device")
+    return x.data_ptr()
 
 
-def _dtype_of(x, where):
-    import torch
-
-    if x.dtype == torch.float32:
-        return CB_F32
-    if x.dtype == torch.bfloat16:
+def _float_kind(x, where):
+    if x.dtype is _torch.bfloat16:
         return CB_BF16
-    raise CBError(-3, f"{where}: {x.dtype}")
+    if x.dtype is _torch.float32:
+        return CB_F32
+    _refuse(where, x, "float32 or bfloat16 is wanted", -3)
 
 
-def _strided(x, where):
+def _row_strides(x, where, dev):
     """Strides of all axes but the last, whose values have to be contiguous."""
-    if x.shape[-1] > 1 and x.stride(-1) != 1:
-        raise CBError(-2, f"{where}: the values of a row are not contiguous")
-    return (_i64 * (x.dim() - 1))(*x.stride()[:-1])
+    if x.get_device() != dev:
+        _refuse(where, x, "not on the current device")
+    st = x.stride()
+    if st[-1] != 1 and x.shape[-1] > 1:
+        _refuse(where, x, "the values of a row are not contiguous")
+    return st[:-1]
 
 
 def cb_rotary_frequencies(rotary_dim: int, base: float = 10000.0, scaling: str = "none",
@@ -469,25 +482,30 @@ def rows(x, out, pos, frm=None) -> cb_rows:
     """Rows of one tensor for cb_rotary: x and out [a][b][c][D] (out may be x), int32 positions
     `pos` and earlier ones `frm` of shapes that broadcast to [a][b][c].  The struct keeps its
     tensors."""
-    import torch
-
-    where = "rows"
-    _tensor(x, where, (torch.float32, torch.bfloat16), 4)
-    _tensor(out, where, (x.dtype,), 4, x.shape)
-    r = cb_rows(x=x.data_ptr(), out=out.data_ptr(), size=(_i64 * 3)(*x.shape[:3]),
-                in_stride=_strided(x, where), out_stride=_strided(out, where))
+    where, torch = "rows", _torch or _lazy_torch()
+    dev = torch.cuda.current_device()
+    kind = _float_kind(x, where)
+    if x.dim() != 4 or out.shape != x.shape:
+        _refuse(where, out, f"rows [a][b][c][D] and their like are wanted, {tuple(x.shape)} given")
+    if out.dtype is not x.dtype:
+        _refuse(where, out, f"{x.dtype} is wanted", -3)
+    r = cb_rows(x=x.data_ptr(), out=out.data_ptr(), size=_S3(*x.shape[:3]),
+                in_stride=_S3(*_row_strides(x, where, dev)),
+                out_stride=_S3(*_row_strides(out, where, dev)))
     r.tensors = (x, out, pos, frm)
-    r.dtype, r.head_dim = _dtype_of(x, where), x.shape[3]
+    r.kind, r.head_dim = kind, x.shape[3]
     for p, name, stride in ((pos, "pos", "pos_stride"), (frm, "frm", "from_stride")):
         if p is not None:
-            _tensor(p, where, (torch.int32,))
+            if p.dtype is not torch.int32:
+                _refuse(where, p, "int32 positions are wanted", -3)
+            if p.get_device() != dev:
+                _refuse(where, p, "not on the current device")
             try:
                 q = p.expand(x.shape[:3])
             except RuntimeError:
-                raise CBError(-2, f"{where}: positions {tuple(p.shape)} for rows "
-                                  f"{tuple(x.shape[:3])}") from None
+                _refuse(where, p, f"positions do not fit rows {tuple(x.shape[:3])}")
             setattr(r, name, q.data_ptr())
-            setattr(r, stride, (_i64 * 3)(*q.stride()))
+            setattr(r, stride, _S3(*q.stride()))
     return r
 
 
@@ -495,40 +513,46 @@ def cb_rotary(parts, freq, amplitude: float = 1.0, interleaved: bool = False,
               transpose: bool = False, stream=None) -> None:
     """Rotates the rows of one or two tensors (`rows`) by the frequencies `freq` (device, float64,
     one a pair)."""
-    import torch
-
-    parts = [parts] if isinstance(parts, cb_rows) else list(parts)
-    _tensor(freq, "cb_rotary", (torch.float64,), 1)
-    if not freq.is_contiguous():
-        raise CBError(-2, "cb_rotary: freq not contiguous")
-    if not 1 <= len(parts) <= 2:
-        raise CBError(-2, "cb_rotary: one or two tensors")
-    if any(p.dtype != parts[0].dtype or p.head_dim != parts[0].head_dim for p in parts):
-        raise CBError(-3, "cb_rotary: parts of unlike types or widths")
-    a = parts[0] if len(parts) == 1 else (cb_rows * 2)(*parts)
-    _check(_lib.cb_rotary(a if len(parts) == 2 else ctypes.byref(a), len(parts), parts[0].head_dim,
-                          freq.data_ptr(), 2 * freq.numel(), float(amplitude), int(interleaved),
-                          int(transpose), parts[0].dtype, _stream(stream)), "cb_rotary")
+    where = "cb_rotary"
+    if isinstance(parts, cb_rows):
+        parts = (parts,)
+    n = len(parts)
+    if not 1 <= n <= 2:
+        raise CBError(-2, f"{where}: one or two tensors")
+    a = parts[0]
+    if n == 2:
+        if parts[1].kind != a.kind:
+            raise CBError(-3, f"{where}: tensors of unlike types")
+        if parts[1].head_dim != a.head_dim:
+            raise CBError(-2, f"{where}: rows of unlike widths")
+    dev, s = _now(stream)
+    if freq.dtype is not _torch.float64:
+        _refuse(where, freq, "float64 frequencies are wanted", -3)
+    if freq.dim() != 1 or not freq.is_contiguous() or freq.get_device() != dev:
+        _refuse(where, freq, "a contiguous list on the current device is wanted")
+    _check(_lib.cb_rotary((cb_rows * 2)(*parts) if n == 2 else _byref(a), n, a.head_dim,
+                          freq.data_ptr(), 2 * freq.shape[0], amplitude, interleaved, transpose,
+                          a.kind, s), where)
 
 
 def cache(pool, refs, table, lens, head_dim: int, page_len: int) -> cb_cache:
     """Descriptor of a paged four-bit cache over the caller's tensors: pool uint8
     [pages][layers][kv_heads][unit], int32 refs [pages], table [seqs][width], lens [seqs].  It keeps
     them."""
-    import torch
-
-    where, D, P = "cache", int(head_dim), int(page_len)
-    _tensor(pool, where, (torch.uint8,), 4, (None, None, None, P * (D + D // 16)))
-    _tensor(refs, where, (torch.int32,), 1, (pool.shape[0],))
-    _tensor(table, where, (torch.int32,), 2)
-    _tensor(lens, where, (torch.int32,), 1, (table.shape[0],))
-    for t in (pool, refs, table, lens):
-        if not t.is_contiguous():
-            raise CBError(-2, f"{where}: not contiguous")
+    where, D, P, torch = "cache", int(head_dim), int(page_len), _torch or _lazy_torch()
+    dev = torch.cuda.current_device()
+    if pool.dtype is not torch.uint8 or table.dtype is not torch.int32:
+        _refuse(where, pool, f"a uint8 pool and int32 tables are wanted, {table.dtype} given", -3)
+    if pool.dim() != 4 or pool.shape[3] != P * (D + D // 16) or table.dim() != 2:
+        _refuse(where, pool, f"a pool [pages][layers][kv_heads][{P * (D + D // 16)}] is wanted")
+    for t in (pool, table):
+        if not t.is_contiguous() or t.get_device() != dev:
+            _refuse(where, t, "not contiguous on the current device")
     c = cb_cache(pool.shape[1], pool.shape[2], D, P, pool.shape[0], table.shape[0], table.shape[1],
-                 0, pool.data_ptr(), refs.data_ptr(), table.data_ptr(), lens.data_ptr())
+                 0, pool.data_ptr(), _ints(refs, where, dev, pool.shape[0]), table.data_ptr(),
+                 _ints(lens, where, dev, table.shape[0]))
     c.tensors = (pool, refs, table, lens)
-    if _lib.cb_cache_page_bytes(ctypes.byref(c)) == 0:
+    if _lib.cb_cache_page_bytes(_byref(c)) == 0:
         raise CBError(-2, where)
     return c
 
@@ -551,75 +575,83 @@ class Cache:
 
 
 def cb_cache_page_bytes(c: cb_cache) -> int:
-    return _lib.cb_cache_page_bytes(ctypes.byref(c))
+    return _lib.cb_cache_page_bytes(_byref(c))
 
 
 def cb_cache_status(status, stream=None) -> int:
     """Synchronises the stream and returns 0 (CB_OK), -9 (CB_ERR_PAGES: pages lacked) or -2
     (CB_ERR_SHAPE: an invalid entry) for the last call that wrote `status`."""
-    return _lib.cb_cache_status(_ptr(_ints(status, "cb_cache_status", 1)), _stream(stream))
+    dev, s = _now(stream)
+    return _lib.cb_cache_status(_ints(status, "cb_cache_status", dev, 1), s)
 
 
 def cb_cache_extend(c: cb_cache, seqs, add, status, stream=None) -> None:
-    n = _ints(seqs, "cb_cache_extend").numel()
-    _check(_lib.cb_cache_extend(ctypes.byref(c), _ptr(seqs), _ptr(_ints(add, "cb_cache_extend", n)), n,
-                                _ptr(_ints(status, "cb_cache_extend", 1)), _stream(stream)),
-           "cb_cache_extend")
+    where = "cb_cache_extend"
+    dev, s = _now(stream)
+    n = seqs.numel()
+    _check(_lib.cb_cache_extend(_byref(c), _ints(seqs, where, dev), _ints(add, where, dev, n), n,
+                                _ints(status, where, dev, 1), s), where)
 
 
 def cb_cache_free(c: cb_cache, seqs, stream=None) -> None:
-    n = _ints(seqs, "cb_cache_free").numel()
-    _check(_lib.cb_cache_free(ctypes.byref(c), _ptr(seqs), n, _stream(stream)), "cb_cache_free")
+    where = "cb_cache_free"
+    dev, s = _now(stream)
+    _check(_lib.cb_cache_free(_byref(c), _ints(seqs, where, dev), seqs.numel(), s), where)
 
 
 def cb_cache_fork_workspace_bytes(c: cb_cache, n: int) -> int:
-    return _lib.cb_cache_fork_workspace_bytes(ctypes.byref(c), int(n))
+    return _lib.cb_cache_fork_workspace_bytes(_byref(c), n)
 
 
 def cb_cache_fork(c: cb_cache, parents, children, status, ws, copy: bool = False, ws_bytes=None,
                   stream=None) -> None:
-    n = _ints(parents, "cb_cache_fork").numel()
-    _ints(children, "cb_cache_fork", n)
-    _check(_lib.cb_cache_fork(ctypes.byref(c), _ptr(parents), _ptr(children), n, int(copy),
-                              _ptr(_ints(status, "cb_cache_fork", 1)), _ptr(ws),
-                              _nbytes(ws, ws_bytes), _stream(stream)), "cb_cache_fork")
+    where = "cb_cache_fork"
+    dev, s = _now(stream)
+    n = parents.numel()
+    _check(_lib.cb_cache_fork(_byref(c), _ints(parents, where, dev), _ints(children, where, dev, n),
+                              n, copy, _ints(status, where, dev, 1), _ptr(ws), _nbytes(ws, ws_bytes),
+                              s), where)
 
 
 def cb_cache_compact_workspace_bytes(c: cb_cache, n: int) -> int:
-    return _lib.cb_cache_compact_workspace_bytes(ctypes.byref(c), int(n))
+    return _lib.cb_cache_compact_workspace_bytes(_byref(c), n)
 
 
 def cb_cache_compact(c: cb_cache, src, dst, idx, status, ws, counts=None, ws_bytes=None,
                      stream=None) -> None:
     """idx: int32 [n][layers or 1][kv_heads or 1][keep]; an axis of one serves all."""
-    import torch
-
     where = "cb_cache_compact"
-    n = _ints(src, where).numel()
-    _ints(dst, where, n)
-    _ints(counts, where, n)
-    _tensor(idx, where, (torch.int32,), 4)
-    if idx.shape[3] > 1 and idx.stride(3) != 1:
-        raise CBError(-2, f"{where}: a list of positions is not contiguous")
-    try:
-        full = idx.expand(n, c.layers, c.kv_heads, idx.shape[3])
-    except RuntimeError:
-        raise CBError(-2, f"{where}: lists {tuple(idx.shape)}") from None
-    _check(_lib.cb_cache_compact(ctypes.byref(c), _ptr(src), _ptr(dst), n, _ptr(idx),
-                                 (_i64 * 3)(*full.stride()[:3]), idx.shape[3], _ptr(counts),
-                                 _ptr(_ints(status, where, 1)), _ptr(ws), _nbytes(ws, ws_bytes),
-                                 _stream(stream)), where)
+    dev, s = _now(stream)
+    n = src.numel()
+    if idx.dtype is not _torch.int32:
+        _refuse(where, idx, "int32 positions are wanted", -3)
+    shape = idx.shape
+    if len(shape) != 4 or shape[0] != n or shape[1] not in (1, c.layers) or \
+            shape[2] not in (1, c.kv_heads):
+        _refuse(where, idx, f"lists [{n}][{c.layers} or 1][{c.kv_heads} or 1][keep] are wanted")
+    st = _row_strides(idx, where, dev)
+    stride = _S3(st[0], 0 if shape[1] == 1 else st[1], 0 if shape[2] == 1 else st[2])
+    _check(_lib.cb_cache_compact(_byref(c), _ints(src, where, dev), _ints(dst, where, dev, n), n,
+                                 idx.data_ptr(), stride, shape[3], _ints(counts, where, dev, n),
+                                 _ints(status, where, dev, 1), _ptr(ws), _nbytes(ws, ws_bytes), s),
+           where)
 
 
 def _cache_rows(fn, where, c, k, v, seqs, start, counts, layer, stream):
-    _tensor(k, where, None, 5, (None, None, c.kv_heads, None, c.head_dim))
-    _tensor(v, where, (k.dtype,), 5, k.shape)
-    if k.stride() != v.stride():
-        raise CBError(-2, f"{where}: keys and values of unlike strides")
-    L, n, _, T, _ = k.shape
-    lists = [_ptr(_ints(x, where, n)) for x in (seqs, start, counts)]
-    _check(fn(ctypes.byref(c), int(layer), L, lists[0], n, lists[1], lists[2], T, k.data_ptr(),
-              v.data_ptr(), _strided(k, where), _dtype_of(k, where), _stream(stream)), where)
+    dev, s = _now(stream)
+    kind, shape = _float_kind(k, where), k.shape
+    if len(shape) != 5 or shape[2] != c.kv_heads or shape[4] != c.head_dim or v.shape != shape:
+        _refuse(where, v, f"rows [layers][n][{c.kv_heads}][rows][{c.head_dim}] are wanted, keys and "
+                          f"values alike, {tuple(shape)} given")
+    if v.dtype is not k.dtype:
+        _refuse(where, v, f"{k.dtype} is wanted", -3)
+    st = _row_strides(k, where, dev)
+    if _row_strides(v, where, dev) != st:
+        _refuse(where, v, "keys and values of unlike strides")
+    n = shape[1]
+    _check(fn(_byref(c), layer, shape[0], _ints(seqs, where, dev, n), n, _ints(start, where, dev, n),
+              _ints(counts, where, dev, n), shape[3], k.data_ptr(), v.data_ptr(), _S4(*st), kind, s),
+           where)
 
 
 def cb_cache_write(c: cb_cache, k, v, seqs=None, start=None, counts=None, layer: int = 0,
@@ -637,30 +669,31 @@ def cb_cache_read(c: cb_cache, k, v, seqs=None, start=None, counts=None, layer: 
 def cb_cache_attend_workspace_bytes(c: cb_cache, layers: int, n: int, q_heads: int,
                                     q_len: int) -> int:
     """Scratch bytes of cb_cache_attend (0: it needs none)."""
-    return _lib.cb_cache_attend_workspace_bytes(ctypes.byref(c), int(layers), int(n), int(q_heads),
-                                                int(q_len))
+    return _lib.cb_cache_attend_workspace_bytes(_byref(c), layers, n, q_heads, q_len)
 
 
 def cb_cache_attend(c: cb_cache, q, out, ws=None, lse=None, seqs=None, q_lens=None,
                     causal: bool = True, scale: float = 0.0, layer: int = 0, ws_bytes=None,
                     stream=None) -> None:
     """q, out [layers][n][q_heads][q_len][D]; lse [layers][n][q_heads][q_len] fp32."""
-    import torch
-
     where = "cb_cache_attend"
-    _tensor(q, where, None, 5, (None, None, None, None, c.head_dim))
-    _tensor(out, where, (q.dtype,), 5, q.shape)
-    L, n, Hq, m, _ = q.shape
-    if lse is not None:
-        _tensor(lse, where, (torch.float32,), 4, q.shape[:4])
-        if not lse.is_contiguous():
-            raise CBError(-2, f"{where}: lse not contiguous")
-    _check(_lib.cb_cache_attend(ctypes.byref(c), int(layer), L, _ptr(_ints(seqs, where, n)), n,
-                                q.data_ptr(), _strided(q, where), Hq,
-                                _ptr(_ints(q_lens, where, n)), m, int(causal), float(scale),
-                                out.data_ptr(), _strided(out, where), _ptr(lse),
-                                _dtype_of(q, where), _ptr(ws), _nbytes(ws, ws_bytes),
-                                _stream(stream)), where)
+    dev, s = _now(stream)
+    kind, shape = _float_kind(q, where), q.shape
+    if len(shape) != 5 or shape[4] != c.head_dim or out.shape != shape:
+        _refuse(where, out, f"rows [layers][n][q_heads][q_len][{c.head_dim}] and their like are wanted, "
+                            f"{tuple(shape)} given")
+    if out.dtype is not q.dtype:
+        _refuse(where, out, f"{q.dtype} is wanted", -3)
+    qs, os_ = _row_strides(q, where, dev), _row_strides(out, where, dev)
+    if lse is not None and (lse.dtype is not _torch.float32 or lse.shape != shape[:4] or
+                            not lse.is_contiguous() or lse.get_device() != dev):
+        _refuse(where, lse, f"contiguous float32 {tuple(shape[:4])} on the current device is wanted")
+    n = shape[1]
+    _check(_lib.cb_cache_attend(_byref(c), layer, shape[0], _ints(seqs, where, dev, n), n,
+                                q.data_ptr(), _S4(*qs), shape[2], _ints(q_lens, where, dev, n),
+                                shape[3], causal, scale, out.data_ptr(), _S4(*os_),
+                                None if lse is None else lse.data_ptr(), kind, _ptr(ws),
+                                _nbytes(ws, ws_bytes), s), where)
 
 
 __all__ = ["cb_layout", "layout", "layout_of", "cb_score_workspace_bytes", "cb_score",
