@@ -136,7 +136,7 @@ int cb_cache_status(const int32_t* status, void* stream);
 /* Room for add[i] (>= 0) more positions behind those of sequence seqs[i]:
  * takes the pages they need and adds add[i] to its length.  All or nothing;
  * invalid: a sequence outside the table or listed twice, add[i] < 0, a length
- * over width * page_len.  One workgroup; n <= 8192. */
+ * over width * page_len.  One workgroup; n <= 2048. */
 int cb_cache_extend(const cb_cache* c, const int32_t* seqs, const int32_t* add, int32_t n,
                     int32_t* status, void* stream);
 
@@ -150,7 +150,7 @@ int cb_cache_free(const cb_cache* c, const int32_t* seqs, int32_t n, void* strea
  * part (so that each side can append); copy != 0: a copy of every page.  Pages
  * that a child held before are given back first.  All or nothing; invalid: an
  * entry outside the table, a child listed twice or that is also a parent.
- * n <= 8192.  ws: cb_cache_fork_workspace_bytes(c, n) bytes, 16-byte aligned. */
+ * n <= 2048.  ws: cb_cache_fork_workspace_bytes(c, n) bytes, 16-byte aligned. */
 size_t cb_cache_fork_workspace_bytes(const cb_cache* c, int32_t n);
 int cb_cache_fork(const cb_cache* c, const int32_t* parents, const int32_t* children, int32_t n,
                   int32_t copy, int32_t* status, void* ws, size_t ws_bytes, void* stream);
@@ -164,7 +164,7 @@ int cb_cache_fork(const cb_cache* c, const int32_t* parents, const int32_t* chil
  * that dst[i] held before are given back.  The rest of the last page is cleared.
  * All or nothing; invalid: an entry outside the table, a dst listed twice or
  * that is the src of another entry, a count below 0 or over keep.
- * 1 <= keep <= width * page_len, n <= 8192. */
+ * 1 <= keep <= width * page_len, n <= 2048. */
 size_t cb_cache_compact_workspace_bytes(const cb_cache* c, int32_t n);
 int cb_cache_compact(const cb_cache* c, const int32_t* src, const int32_t* dst, int32_t n,
                      const int32_t* idx, const int64_t idx_stride[3], int64_t keep,

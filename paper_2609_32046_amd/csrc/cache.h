@@ -6,7 +6,7 @@
 
 namespace cb {
 
-constexpr int kCacheMaxEntries = 8192;     // entries of a page call
+constexpr int kCacheMaxEntries = 2048;     // entries of a page call: their lists lie in LDS
 constexpr int kCacheMaxSeqs = 1 << 17;     // its bit set of sequences fills 16 KiB of LDS
 constexpr int kCacheMaxPages = 1 << 24;
 

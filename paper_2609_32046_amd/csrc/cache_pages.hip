@@ -13,11 +13,11 @@ namespace cb {
 namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kPlan = 1024;         // threads of a planning workgroup
 constexpr int kPlanWaves = kPlan / 64;
-constexpr int kScan = 4;            // 16-byte reads of refs a thread has under way
+constexpr int kScan = 16;           // reads of refs a thread has under way
+constexpr int kItems = 4;           // pages of rows a thread has under way
 
 __device__ inline int held_pages(const CacheView& c, int len) {
   const int64_t n = ((int64_t)(len > 0 ? len : 0) + (1 << c.page_shift) - 1) >> c.page_shift;
@@ -73,12 +73,38 @@ __device__ inline bool marked(const uint32_t* bits, int seq) {
   return (bits[seq >> 5] >> (seq & 31)) & 1u;
 }
 
+// A list of sequences with their lengths, in LDS: the rows' pages are then one read away.
+struct SeqList {
+  int seq[kCacheMaxEntries];
+  int len[kCacheMaxEntries];
+  int most;   // pages of the longest
+};
+
 struct PlanShared {
   int sums[kPlanWaves];
+  int rows[kScan * kPlanWaves];
+  int free;
   int bad;
-  int found;
   int offset[kCacheMaxEntries + 1];   // pages that the entries before need
 };
+
+// Fills a list (a barrier follows); entries outside the table get no pages.  Returns
+// whether one of this thread's is outside.
+__device__ inline bool fill_list(const CacheView& c, SeqList& l, const int32_t* seqs, int n) {
+  bool bad = false;
+  int most = 0;
+  for (int i = threadIdx.x; i < n; i += kPlan) {
+    const int s = seqs[i];
+    const int len = known(c, s) ? c.lens[s] : 0;
+    bad |= !known(c, s) || len < 0;
+    l.seq[i] = s;
+    l.len[i] = len;
+    const int k = held_pages(c, len);
+    most = k > most ? k : most;
+  }
+  if (most > 0) atomicMax(&l.most, most);
+  return bad;
+}
 
 // Gives a page back; a count that was zero (a page listed by mistake) stays.
 __device__ inline void drop(int32_t* refs, int page) {
@@ -102,44 +128,88 @@ __device__ inline int64_t plan_offsets(PlanShared& sh, int n, Need need) {
   return base;
 }
 
-// Calls take(page, rank) for the free pages of lowest number, ranks 0..want-1
-// in order of their numbers, and returns how many there are (at most want).  refs are read
-// with device scope: this workgroup's own atomics have changed them.
-template <typename Take>
-__device__ inline int64_t scan_free(const CacheView& c, PlanShared& sh, int64_t want, Take take) {
-  int64_t base = 0;
-  constexpr int kStep = kPlan * 4 * kScan;
-  for (int64_t p0 = 0; p0 < c.pages && base < want; p0 += kStep) {
-    // thread i holds pages p0 + (j * kPlan + i) * 4 ..: every j a contiguous piece
-    i32x4 r[kScan];
+// One sweep over kScan rows of kPlan pages, a page of each row to a thread: free pages
+// that lie together, as the lowest do, then fall to different threads, which
+// enter them in their rows at the same time.
+struct Sweep {
+  uint32_t free;   // bit j: this thread's page of row j is free
+  int64_t p0;
+  // Ranks within the sweep go through sh.rows; returns how many pages are free.
+  __device__ int load(const CacheView& c, PlanShared& sh, int64_t from) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    p0 = from + threadIdx.x;
+    int r[kScan];
+#pragma unroll
+    for (int j = 0; j < kScan; ++j)
+      r[j] = p0 + j * kPlan < c.pages ? c.refs[p0 + j * kPlan] : 1;
+    free = 0;
+    __syncthreads();   // the last sweep's ranks have been read
 #pragma unroll
     for (int j = 0; j < kScan; ++j) {
-      const int64_t p = p0 + ((int64_t)j * kPlan + threadIdx.x) * 4;
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        r[j][e] = p + e < c.pages ? __hip_atomic_load(&c.refs[p + e], __ATOMIC_RELAXED,
-                                                       __HIP_MEMORY_SCOPE_AGENT)
-                                  : 1;
+      free |= r[j] == 0 ? 1u << j : 0u;
+      const uint64_t b = __ballot(r[j] == 0);
+      if (lane == 0) sh.rows[j * kPlanWaves + wave] = __popcll(b);
     }
+    __syncthreads();
+    // exclusive prefixes of the kScan * kPlanWaves counts, by the first wave
+    constexpr int kEach = kScan * kPlanWaves / 64;
+    if (wave == 0) {
+      int v[kEach], sum = 0;
 #pragma unroll
+      for (int k = 0; k < kEach; ++k) {
+        v[k] = sh.rows[lane * kEach + k];
+        sum += v[k];
+      }
+      int at = wave_scan(sum) - sum;
+#pragma unroll
+      for (int k = 0; k < kEach; ++k) {
+        sh.rows[lane * kEach + k] = at;
+        at += v[k];
+      }
+      if (lane == 63) sh.free = at;
+    }
+    __syncthreads();
+    return sh.free;
+  }
+  // take(page, rank) for this thread's free pages of rank below want; base: free pages before
+  // the sweep.
+  template <typename Take>
+  __device__ void give(const PlanShared& sh, int64_t base, int64_t want, Take take) const {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll 1
     for (int j = 0; j < kScan; ++j) {
-      int mine = 0;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) mine += r[j][e] == 0;
-      int total;
-      int64_t rank = base + group_scan(mine, sh.sums, &total);
-      const int64_t p = p0 + ((int64_t)j * kPlan + threadIdx.x) * 4;
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (r[j][e] == 0) {
-          if (rank < want) take((int)(p + e), (int)rank);
-          ++rank;
-        }
-      base += total;
-      if (base >= want) break;   // the same in every thread
+      const bool is = (free >> j) & 1u;
+      const uint64_t b = __ballot(is);
+      const int64_t rank =
+          base + sh.rows[j * kPlanWaves + wave] + __popcll(b & ((1ull << lane) - 1));
+      if (is && rank < want) take((int)(p0 + j * kPlan), (int)rank);
     }
   }
-  return base < want ? base : want;
+};
+
+// Calls take(page, rank) for the `want` free pages of lowest number, ranks in order of
+// their numbers, if there are so many; returns how many there are, at most want.  The
+// caller has fenced its own changes to refs.
+template <typename Take>
+__device__ inline int64_t take_free(const CacheView& c, PlanShared& sh, int64_t want, Take take) {
+  constexpr int kStep = kPlan * kScan;
+  Sweep sw;
+  int64_t base = sw.load(c, sh, 0);
+  if (base >= want) {   // within the first sweep: no second look
+    sw.give(sh, 0, want, take);
+    return want;
+  }
+  int64_t p0 = kStep;
+  for (; p0 < c.pages && base < want; p0 += kStep) base += sw.load(c, sh, p0);
+  if (base < want) return base;
+  const int64_t end = p0;
+  base = 0;
+  for (p0 = 0; p0 < end; p0 += kStep) {
+    const int k = sw.load(c, sh, p0);
+    sw.give(sh, base, want, take);
+    base += k;
+  }
+  return want;
 }
 
 // Entry whose pages include rank r.
@@ -153,6 +223,9 @@ __device__ inline int entry_of(const PlanShared& sh, int n, int r) {
   return lo;
 }
 
+// What *status says where pages lack.
+__device__ inline int lacking(int64_t k) { return (int)(k < 0x7fffffff ? k : 0x7fffffff); }
+
 __device__ inline void clear_bits(uint32_t* bits, int seqs) {
   for (int i = threadIdx.x; i < (seqs + 31) / 32; i += kPlan) bits[i] = 0u;
 }
@@ -165,38 +238,33 @@ __global__ __launch_bounds__(kPlan) void cache_extend_kernel(CacheView c,
                                                              int n, int32_t* status) {
   extern __shared__ uint32_t bits[];
   __shared__ PlanShared sh;
+  __shared__ SeqList l;
   clear_bits(bits, c.seqs);
-  if (threadIdx.x == 0) sh.bad = 0;
+  if (threadIdx.x == 0) sh.bad = l.most = 0;
   __syncthreads();
   const int64_t room = (int64_t)c.width << c.page_shift;
-  for (int i = threadIdx.x; i < n; i += kPlan) {
-    const int s = seqs[i];
-    if (!known(c, s) || mark(bits, s) || add[i] < 0 || c.lens[s] < 0 ||
-        (int64_t)c.lens[s] + add[i] > room)
-      sh.bad = 1;
-  }
+  bool bad = fill_list(c, l, seqs, n);
+  for (int i = threadIdx.x; i < n; i += kPlan)   // this thread's own entries
+    bad |= (known(c, l.seq[i]) && mark(bits, l.seq[i])) || add[i] < 0 ||
+           (int64_t)l.len[i] + add[i] > room;
+  if (bad) sh.bad = 1;
   __syncthreads();
   if (sh.bad) {
     if (threadIdx.x == 0) *status = -1;
     return;
   }
-  const int64_t want = plan_offsets(sh, n, [&](int i) {
-    const int len = c.lens[seqs[i]];
-    return held_pages(c, len + add[i]) - held_pages(c, len);
-  });
-  const int64_t have = scan_free(c, sh, want, [](int, int) {});
-  if (have < want) {
-    if (threadIdx.x == 0) *status = (int)(want - have < 0x7fffffff ? want - have : 0x7fffffff);
-    return;
-  }
-  scan_free(c, sh, want, [&](int page, int rank) {
+  const int64_t want = plan_offsets(
+      sh, n, [&](int i) { return held_pages(c, l.len[i] + add[i]) - held_pages(c, l.len[i]); });
+  const int64_t have = take_free(c, sh, want, [&](int page, int rank) {
     const int i = entry_of(sh, n, rank);
-    const int s = seqs[i];
-    c.table[(int64_t)s * c.width + held_pages(c, c.lens[s]) + rank - sh.offset[i]] = page;
+    c.table[(int64_t)l.seq[i] * c.width + held_pages(c, l.len[i]) + rank - sh.offset[i]] = page;
     c.refs[page] = 1;
   });
-  __syncthreads();   // lens are read above
-  for (int i = threadIdx.x; i < n; i += kPlan) c.lens[seqs[i]] += add[i];
+  if (have < want) {
+    if (threadIdx.x == 0) *status = lacking(want - have);
+    return;
+  }
+  for (int i = threadIdx.x; i < n; i += kPlan) c.lens[l.seq[i]] = l.len[i] + add[i];
   if (threadIdx.x == 0) *status = 0;
 }
 
@@ -216,21 +284,33 @@ __global__ __launch_bounds__(256) void cache_free_kernel(CacheView c,
   }
 }
 
-// Adds d to the holders of every page of the listed sequences (release: -1,
-// taking back: +1).  Rows of table, one wave each.
-__device__ inline void add_refs(const CacheView& c, const int32_t* seqs, int n, int d,
-                                const int32_t* unless) {
-  const int lane = threadIdx.x & 63;
-  for (int i = threadIdx.x >> 6; i < n; i += kPlanWaves) {
-    const int s = seqs[i];
-    if (unless && unless[i] == s) continue;
-    const int pages = held_pages(c, c.lens[s]);
-    for (int j = lane; j < pages; j += 64) {
-      const int p = c.table[(int64_t)s * c.width + j];
-      if ((unsigned)p < (unsigned)c.pages) atomicAdd(&c.refs[p], d);
+// f(i, j, page) for the pages j of the listed sequences' rows as they stand, kItems of
+// them under way in every thread: a row is short, and a row at a time would be all latency.
+template <typename F>
+__device__ inline void each_page(const CacheView& c, const SeqList& l, int n, F f) {
+  // a row's pages are dealt to the next power of two of threads, 16 to 1024
+  int shift = 4;
+  while ((1 << shift) < l.most && shift < 10) ++shift;
+  const int lane = threadIdx.x & ((1 << shift) - 1);
+  for (int j0 = 0; j0 < l.most; j0 += 1 << shift) {
+    const int j = j0 + lane;
+    for (int i0 = threadIdx.x >> shift; i0 < n; i0 += kItems * (kPlan >> shift)) {
+      int page[kItems];
+#pragma unroll
+      for (int e = 0; e < kItems; ++e) {
+        const int i = i0 + e * (kPlan >> shift);
+        page[e] = i < n && j < held_pages(c, l.len[i]) ? c.table[(int64_t)l.seq[i] * c.width + j] : -1;
+      }
+#pragma unroll
+      for (int e = 0; e < kItems; ++e) {
+        const int i = i0 + e * (kPlan >> shift);
+        if (i < n && j < held_pages(c, l.len[i])) f(i, j, page[e]);
+      }
     }
   }
 }
+
+__device__ inline bool is_page(const CacheView& c, int p) { return (unsigned)p < (unsigned)c.pages; }
 
 // ws of a fork: how many pages are copied (padded to 16 bytes), then (from, to).
 __global__ __launch_bounds__(kPlan) void cache_fork_kernel(CacheView c,
@@ -240,72 +320,68 @@ __global__ __launch_bounds__(kPlan) void cache_fork_kernel(CacheView c,
                                                            int32_t* count, int2* pairs) {
   extern __shared__ uint32_t bits[];
   __shared__ PlanShared sh;
-  const int lane = threadIdx.x & 63;
+  __shared__ SeqList from, to;
   clear_bits(bits, c.seqs);
   if (threadIdx.x == 0) {
-    sh.bad = 0;
+    sh.bad = from.most = to.most = 0;
     *count = 0;
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < n; i += kPlan)
-    if (!known(c, parents[i]) || !known(c, children[i]) || mark(bits, children[i])) sh.bad = 1;
+  bool bad = fill_list(c, from, parents, n);
+  bad |= fill_list(c, to, children, n);
+  for (int i = threadIdx.x; i < n; i += kPlan)   // this thread's own entries
+    bad |= known(c, to.seq[i]) && mark(bits, to.seq[i]);
+  if (bad) sh.bad = 1;
   __syncthreads();
   for (int i = threadIdx.x; i < n; i += kPlan)
-    if (known(c, parents[i]) && marked(bits, parents[i])) sh.bad = 1;
-  __syncthreads();
-  if (!sh.bad)   // every page that a parent says it holds is one
-    for (int i = threadIdx.x >> 6; i < n; i += kPlanWaves) {
-      const int s = parents[i], pages = held_pages(c, c.lens[s]);
-      for (int j = lane; j < pages; j += 64)
-        if ((unsigned)c.table[(int64_t)s * c.width + j] >= (unsigned)c.pages) sh.bad = 1;
-    }
+    if (known(c, from.seq[i]) && marked(bits, from.seq[i])) sh.bad = 1;
   __syncthreads();
   if (sh.bad) {
     if (threadIdx.x == 0) *status = -1;
     return;
   }
-  add_refs(c, children, n, -1, nullptr);
+  // every page that a parent says it holds is one
+  each_page(c, from, n, [&](int, int, int p) {
+    if (!is_page(c, p)) sh.bad = 1;
+  });
+  auto hold = [&](int d) {   // the children's pages
+    each_page(c, to, n, [&](int, int, int p) {
+      if (is_page(c, p)) atomicAdd(&c.refs[p], d);
+    });
+  };
+  hold(-1);
   const int part = (1 << c.page_shift) - 1;
   const int64_t want = plan_offsets(sh, n, [&](int i) {
-    const int len = c.lens[parents[i]];
+    const int len = from.len[i];
     return copy ? held_pages(c, len) : (len > 0 && (len & part) != 0);
   });
   __threadfence();
   __syncthreads();
-  const int64_t have = scan_free(c, sh, want, [](int, int) {});
-  if (have < want) {
-    add_refs(c, children, n, 1, nullptr);
-    if (threadIdx.x == 0) *status = (int)(want - have < 0x7fffffff ? want - have : 0x7fffffff);
-    return;
-  }
-  // which pages are copied, and where to; the children's own rows follow
-  scan_free(c, sh, want, [&](int page, int rank) {
+  // the children's own pages, and what is copied into them
+  const int64_t have = sh.bad ? -1 : take_free(c, sh, want, [&](int page, int rank) {
     const int i = entry_of(sh, n, rank);
-    const int s = parents[i];
-    const int j = copy ? rank - sh.offset[i] : held_pages(c, c.lens[s]) - 1;
-    pairs[rank] = make_int2(c.table[(int64_t)s * c.width + j], page);
+    const int j = copy ? rank - sh.offset[i] : held_pages(c, from.len[i]) - 1;
+    pairs[rank] = make_int2(c.table[(int64_t)from.seq[i] * c.width + j], page);
+    c.table[(int64_t)to.seq[i] * c.width + j] = page;
     c.refs[page] = 1;
   });
-  __threadfence_block();
-  __syncthreads();
-  for (int i = threadIdx.x >> 6; i < n; i += kPlanWaves) {
-    const int s = parents[i], d = children[i];
-    const int len = c.lens[s], pages = held_pages(c, len), before = held_pages(c, c.lens[d]);
-    const int own = sh.offset[i + 1] - sh.offset[i];
-    for (int j = lane; j < pages; j += 64) {
-      int p;
-      if (j >= pages - own) {
-        p = pairs[sh.offset[i] + j - (pages - own)].y;
-      } else {
-        p = c.table[(int64_t)s * c.width + j];
-        atomicAdd(&c.refs[p], 1);
-      }
-      c.table[(int64_t)d * c.width + j] = p;
-    }
-    for (int j = pages + lane; j < before; j += 64) c.table[(int64_t)d * c.width + j] = -1;
+  if (have < want) {
+    hold(1);
+    if (threadIdx.x == 0) *status = have < 0 ? -1 : lacking(want - have);
+    return;
   }
-  __syncthreads();
-  for (int i = threadIdx.x; i < n; i += kPlan) c.lens[children[i]] = c.lens[parents[i]];
+  // the shared ones, and what the children held beyond their new lengths
+  if (!copy)
+    each_page(c, from, n, [&](int i, int j, int p) {
+      if (j < held_pages(c, from.len[i]) - (sh.offset[i + 1] - sh.offset[i])) {
+        atomicAdd(&c.refs[p], 1);
+        c.table[(int64_t)to.seq[i] * c.width + j] = p;
+      }
+    });
+  each_page(c, to, n, [&](int i, int j, int) {
+    if (j >= held_pages(c, from.len[i])) c.table[(int64_t)to.seq[i] * c.width + j] = -1;
+  });
+  for (int i = threadIdx.x; i < n; i += kPlan) c.lens[to.seq[i]] = from.len[i];
   if (threadIdx.x == 0) {
     *status = 0;
     *count = (int)want;
@@ -349,63 +425,64 @@ __device__ inline int64_t kept(const CacheCompactArgs& a, int i) {
 __global__ __launch_bounds__(kPlan) void cache_compact_plan_kernel(CacheCompactArgs a) {
   extern __shared__ uint32_t bits[];
   __shared__ PlanShared sh;
+  __shared__ SeqList from, to;
   const CacheView& c = a.c;
-  const int lane = threadIdx.x & 63, n = a.n;
+  const int n = a.n;
   clear_bits(bits, c.seqs);
-  if (threadIdx.x == 0) sh.bad = 0;
+  if (threadIdx.x == 0) sh.bad = from.most = to.most = 0;
   __syncthreads();
-  for (int i = threadIdx.x; i < n; i += kPlan) {
+  bool bad = fill_list(c, from, a.src, n);
+  bad |= fill_list(c, to, a.dst, n);
+  for (int i = threadIdx.x; i < n; i += kPlan) {   // this thread's own entries
     const int64_t k = kept(a, i);
-    if (!known(c, a.src[i]) || !known(c, a.dst[i]) || k < 0 || k > a.keep ||
-        mark(bits, a.dst[i]))
-      sh.bad = 1;
+    bad |= k < 0 || k > a.keep || (known(c, to.seq[i]) && mark(bits, to.seq[i]));
   }
+  if (bad) sh.bad = 1;
   __syncthreads();
   for (int i = threadIdx.x; i < n; i += kPlan)
-    if (known(c, a.src[i]) && marked(bits, a.src[i]) && a.dst[i] != a.src[i]) sh.bad = 1;
+    if (known(c, from.seq[i]) && marked(bits, from.seq[i]) && to.seq[i] != from.seq[i]) sh.bad = 1;
   __syncthreads();
   if (sh.bad) {
     if (threadIdx.x == 0) *a.status = -1;
     return;
   }
-  add_refs(c, a.dst, n, -1, a.src);   // not those that are read
+  auto hold = [&](int d) {   // what dst held, but for the rows that are read
+    each_page(c, to, n, [&](int i, int, int p) {
+      if (from.seq[i] != to.seq[i] && is_page(c, p)) atomicAdd(&c.refs[p], d);
+    });
+  };
+  hold(-1);
   const int64_t P = 1 << c.page_shift;
   const int64_t want =
       plan_offsets(sh, n, [&](int i) { return (int)((kept(a, i) + P - 1) >> c.page_shift); });
-  __threadfence();
-  __syncthreads();
-  const int64_t have = scan_free(c, sh, want, [](int, int) {});
-  if (have < want) {
-    add_refs(c, a.dst, n, 1, a.src);
-    if (threadIdx.x == 0) *a.status = (int)(want - have < 0x7fffffff ? want - have : 0x7fffffff);
-    return;
-  }
-  for (int i = threadIdx.x >> 6; i < n; i += kPlanWaves) {
-    const int s = a.src[i], len = c.lens[s], pages = held_pages(c, len);
-    int32_t* old = a.old_rows + (int64_t)i * (c.width + 1);
-    if (lane == 0) old[0] = len;
-    for (int j = lane; j < pages; j += 64) old[1 + j] = c.table[(int64_t)s * c.width + j];
-  }
-  __threadfence_block();
-  __syncthreads();
-  scan_free(c, sh, want, [&](int page, int rank) {
-    const int i = entry_of(sh, n, rank);
-    c.table[(int64_t)a.dst[i] * c.width + rank - sh.offset[i]] = page;
-    c.refs[page] = 1;
+  // the sources' rows, before any of them changes
+  for (int i = threadIdx.x; i < n; i += kPlan)
+    a.old_rows[(int64_t)i * (c.width + 1)] = from.len[i];
+  each_page(c, from, n, [&](int i, int j, int p) {
+    a.old_rows[(int64_t)i * (c.width + 1) + 1 + j] = p;
   });
   __threadfence();
   __syncthreads();
-  for (int i = threadIdx.x >> 6; i < n; i += kPlanWaves) {
-    const int d = a.dst[i], before = held_pages(c, c.lens[d]);
-    const int32_t* old = a.old_rows + (int64_t)i * (c.width + 1);
-    for (int j = sh.offset[i + 1] - sh.offset[i] + lane; j < before; j += 64)
-      c.table[(int64_t)d * c.width + j] = -1;
-    if (a.src[i] == d)   // its old pages, which the gather still reads
-      for (int j = lane; j < before; j += 64)
-        if ((unsigned)old[1 + j] < (unsigned)c.pages) drop(c.refs, old[1 + j]);
+  const int64_t have = take_free(c, sh, want, [&](int page, int rank) {
+    const int i = entry_of(sh, n, rank);
+    c.table[(int64_t)to.seq[i] * c.width + rank - sh.offset[i]] = page;
+    c.refs[page] = 1;
+  });
+  if (have < want) {
+    hold(1);
+    if (threadIdx.x == 0) *a.status = lacking(want - have);
+    return;
   }
-  __syncthreads();
-  for (int i = threadIdx.x; i < n; i += kPlan) c.lens[a.dst[i]] = (int)kept(a, i);
+  // what dst held beyond its new length; a source that is its own dst lets its old pages
+  // go, which the gather still reads
+  each_page(c, to, n, [&](int i, int j, int) {
+    if (j >= sh.offset[i + 1] - sh.offset[i]) c.table[(int64_t)to.seq[i] * c.width + j] = -1;
+    if (from.seq[i] == to.seq[i]) {
+      const int p = a.old_rows[(int64_t)i * (c.width + 1) + 1 + j];
+      if (is_page(c, p)) drop(c.refs, p);
+    }
+  });
+  for (int i = threadIdx.x; i < n; i += kPlan) c.lens[to.seq[i]] = (int)kept(a, i);
   if (threadIdx.x == 0) *a.status = 0;
 }
 

@@ -184,10 +184,10 @@ def test_cache_calls_refuse_bad_arguments(cb):
     zero4 = (ctypes.c_int64 * 4)(4096, 2048, 0, 64)
     for name, bad, code in [
             ("extend", dict(seqs=None), -1), ("extend", dict(add=None), -1), ("extend", dict(status=None), -1),
-            ("extend", dict(n=-1), -2), ("extend", dict(n=8193), -2), ("extend", dict(add=FAKE + 2), -6),
+            ("extend", dict(n=-1), -2), ("extend", dict(n=2049), -2), ("extend", dict(add=FAKE + 2), -6),
             ("free", dict(seqs=None), -1), ("free", dict(n=-1), -2), ("free", dict(seqs=FAKE + 1), -6),
             ("fork", dict(parents=None), -1), ("fork", dict(children=None), -1), ("fork", dict(status=None), -1),
-            ("fork", dict(n=8193), -2), ("fork", dict(ws=None), -5), ("fork", dict(ws_bytes=16 + 2 * 4 * 8 - 1), -5),
+            ("fork", dict(n=2049), -2), ("fork", dict(ws=None), -5), ("fork", dict(ws_bytes=16 + 2 * 4 * 8 - 1), -5),
             ("fork", dict(ws=FAKE + 8), -6), ("fork", dict(status=FAKE + 2), -6),
             ("compact", dict(src=None), -1), ("compact", dict(dst=None), -1), ("compact", dict(idx=None), -1),
             ("compact", dict(stride=None), -1), ("compact", dict(keep=0), -2), ("compact", dict(keep=65), -2),
@@ -226,7 +226,7 @@ def test_sizes(cb):
     assert cb._lib.cb_cache_page_bytes(L(desc(cb))) == 2 * 2 * 16 * 68
     assert cb._lib.cb_cache_page_bytes(L(desc(cb, head_dim=128, page_len=64))) == 2 * 2 * 64 * 136
     for fn in (cb._lib.cb_cache_fork_workspace_bytes, cb._lib.cb_cache_compact_workspace_bytes):
-        assert fn(L(desc(cb)), 3) > 0 and fn(L(desc(cb)), -1) == 0 and fn(L(desc(cb)), 8193) == 0
+        assert fn(L(desc(cb)), 3) > 0 and fn(L(desc(cb)), -1) == 0 and fn(L(desc(cb)), 2049) == 0
         assert fn(L(desc(cb, width=0)), 3) == 0
     n = cb._lib.cb_cache_attend_workspace_bytes
     assert n(L(desc(cb)), 1, 1, 4, 1) == 0                       # 64 positions: no split
