@@ -630,47 +630,54 @@ __global__ __launch_bounds__(kThreads, RT == 1 && !F32 ? 3 : 2) void attend_kern
   }
 }
 
-// Rows of sequences that several runs share: a workgroup a row, D/4 lanes a piece of
-// it, 256 / (D/4) pieces at a time, then those in order.
-template <int D, bool F32>
-__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, uint32_t rows_most) {
+// Rows of sequences that several runs share.  SETS groups of D/4 lanes read a row's pieces in
+// turn, then join in order: as many as a workgroup holds where a row has dozens of
+// pieces (one answer's long context), one where it has a few (a prompt's thousands of rows).
+template <int D, bool F32, int SETS>
+__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, uint32_t row_blocks) {
   typedef typename RowType<F32>::type T;
-  constexpr int kLanes = D / 4, kSets = 256 / kLanes, kAhead = 4;
-  __shared__ f32x4 so[kSets][kLanes];
-  __shared__ float2 sml[kSets];
+  constexpr int kLanes = D / 4, kRows = 256 / kLanes / SETS;
+  constexpr int kAhead = SETS > 1 ? 12 : 4;   // pieces under way: 96 runs of a row in one turn
+  __shared__ f32x4 so[SETS][kLanes];
+  __shared__ float2 sml[SETS];
   uint32_t id = blockIdx.x;
-  const int row = (int)(id % rows_most);
-  id /= rows_most;
+  const int set = (int)threadIdx.x / kLanes % SETS;
+  const int row = (int)(id % row_blocks) * kRows + (int)threadIdx.x / (kLanes * SETS);
+  id /= row_blocks;
   const int head = (int)(id % (uint32_t)a.c.heads);
   id /= (uint32_t)a.c.heads;
   const int b = (int)(id % (uint32_t)a.n);
   const int layer = (int)(id / (uint32_t)a.n);
   const int rows = query_tokens(a, b) * a.group;
-  if (row >= rows) return;
+  const bool live = row < rows;
+  if (SETS > 1 && !live) return;   // one row a workgroup
   int64_t total;
   const int64_t per = rounds_per_run(a, &total);
-  const int lane = threadIdx.x & 63;
   int64_t before = 0;
   if (b > 0) {
-    for (int i = lane; i < b; i += 64) before += rounds_of(seq_len(a, i));
+    for (int i = (int)threadIdx.x & 63; i < b; i += 64) before += rounds_of(seq_len(a, i));
     before = uniform64(wave_sum64(before));
   }
   const int64_t first = before / per;
   const int count = (int)((before + rounds_of(seq_len(a, b)) - 1) / per - first) + 1;
-  if (count == 1) return;
-  const int set = threadIdx.x / kLanes, d0 = (threadIdx.x % kLanes) * 4;
+  if (count == 1 || !live) return;
+  const int d0 = ((int)threadIdx.x % kLanes) * 4;
   const int64_t base = ((int64_t)layer * a.c.heads + head) * a.slots + first + b;
   float M = kNone, L = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  for (int k0 = set; k0 < count; k0 += kSets * kAhead) {
+  for (int k0 = set; k0 < count; k0 += SETS * kAhead) {
     float2 ml[kAhead];
     f32x4 x[kAhead];
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
-      const int k = k0 + j * kSets;
-      const int64_t at = (base + (k < count ? k : k0)) * a.rows_pad + row;
-      ml[j] = a.part_ml[at];
-      x[j] = *reinterpret_cast<const f32x4*>(a.part_o + at * D + d0);
+      const int k = k0 + j * SETS;
+      ml[j] = make_float2(kNone, 0.f);
+      x[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (k < count) {
+        const int64_t at = (base + k) * a.rows_pad + row;
+        ml[j] = a.part_ml[at];
+        x[j] = *reinterpret_cast<const f32x4*>(a.part_o + at * D + d0);
+      }
     }
     float next = M;
 #pragma unroll
@@ -680,26 +687,27 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, uint32_t
     acc *= f0;
     M = next;
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j)
-      if (k0 + j * kSets < count) {
-        const float f = ml[j].x == M ? 1.f : __builtin_amdgcn_exp2f(ml[j].x - M);
-        L += ml[j].y * f;
-        acc += x[j] * f;
-      }
+    for (int j = 0; j < kAhead; ++j) {
+      const float f = ml[j].x == M ? 1.f : __builtin_amdgcn_exp2f(ml[j].x - M);
+      L += ml[j].y * f;
+      acc += x[j] * f;
+    }
   }
-  so[set][threadIdx.x % kLanes] = acc;
-  if (d0 == 0) sml[set] = make_float2(M, L);
-  __syncthreads();
-  if (set != 0) return;
+  if constexpr (SETS > 1) {
+    so[set][threadIdx.x % kLanes] = acc;
+    if (d0 == 0) sml[set] = make_float2(M, L);
+    __syncthreads();
+    if (set != 0) return;
 #pragma unroll
-  for (int w = 0; w < kSets; ++w) M = fmaxf(M, sml[w].x);
-  acc = f32x4{0.f, 0.f, 0.f, 0.f};
-  L = 0.f;
+    for (int w = 0; w < SETS; ++w) M = fmaxf(M, sml[w].x);
+    acc = f32x4{0.f, 0.f, 0.f, 0.f};
+    L = 0.f;
 #pragma unroll
-  for (int w = 0; w < kSets; ++w) {
-    const float f = sml[w].x == M ? 1.f : __builtin_amdgcn_exp2f(sml[w].x - M);
-    L += sml[w].y * f;
-    acc += so[w][threadIdx.x] * f;
+    for (int w = 0; w < SETS; ++w) {
+      const float f = sml[w].x == M ? 1.f : __builtin_amdgcn_exp2f(sml[w].x - M);
+      L += sml[w].y * f;
+      acc += so[w][threadIdx.x] * f;
+    }
   }
   const float inv = L == 0.f ? 0.f : 1.f / L;
   const int tok = row / a.group;
@@ -727,10 +735,17 @@ hipError_t launch(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
   else attend_kernel<D, F32, kMost><<<(unsigned)grid, kThreads, 0, s>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.total == 0) return e;   // one run: nothing to join
+  // pieces of a row: about the runs over the sequences
+  constexpr int kRows = 256 / (D / 4);
   const int64_t rows = a.q_len * a.group;
-  const int64_t g2 = rows * a.c.heads * a.n * a.layers;
+  const bool many = a.target >= 8 * (int64_t)a.n;
+  const int64_t blocks = many ? rows : (rows + kRows - 1) / kRows;
+  const int64_t g2 = blocks * a.c.heads * a.n * a.layers;
   if (g2 > 0x7fffffff) return hipErrorInvalidValue;
-  attend_join_kernel<D, F32><<<(unsigned)g2, 256, 0, s>>>(a, (uint32_t)rows);
+  if (many)
+    attend_join_kernel<D, F32, kRows><<<(unsigned)g2, 256, 0, s>>>(a, (uint32_t)blocks);
+  else
+    attend_join_kernel<D, F32, 1><<<(unsigned)g2, 256, 0, s>>>(a, (uint32_t)blocks);
   return hipGetLastError();
 }
 
