@@ -442,6 +442,15 @@ def _ints(x, where, dev, n=None):
     return x.data_ptr()
 
 
+def _scratch(ws, ws_bytes, where, dev):
+    """Address and size of a call's scratch."""
+    if ws is None or isinstance(ws, int):
+        return ws, ws_bytes or 0
+    if ws.get_device() != dev or not ws.is_contiguous():
+        _refuse(where, ws, "scratch is not contiguous on the current device")
+    return ws.data_ptr(), ws.numel() * ws.element_size() if ws_bytes is None else ws_bytes
+
+
 def _float_kind(x, where):
     if x.dtype is _torch.bfloat16:
         return CB_BF16
@@ -609,8 +618,8 @@ def cb_cache_fork(c: cb_cache, parents, children, status, ws, copy: bool = False
     dev, s = _now(stream)
     n = parents.numel()
     _check(_lib.cb_cache_fork(_byref(c), _ints(parents, where, dev), _ints(children, where, dev, n),
-                              n, copy, _ints(status, where, dev, 1), _ptr(ws), _nbytes(ws, ws_bytes),
-                              s), where)
+                              n, copy, _ints(status, where, dev, 1),
+                              *_scratch(ws, ws_bytes, where, dev), s), where)
 
 
 def cb_cache_compact_workspace_bytes(c: cb_cache, n: int) -> int:
@@ -633,8 +642,8 @@ def cb_cache_compact(c: cb_cache, src, dst, idx, status, ws, counts=None, ws_byt
     stride = _S3(st[0], 0 if shape[1] == 1 else st[1], 0 if shape[2] == 1 else st[2])
     _check(_lib.cb_cache_compact(_byref(c), _ints(src, where, dev), _ints(dst, where, dev, n), n,
                                  idx.data_ptr(), stride, shape[3], _ints(counts, where, dev, n),
-                                 _ints(status, where, dev, 1), _ptr(ws), _nbytes(ws, ws_bytes), s),
-           where)
+                                 _ints(status, where, dev, 1), *_scratch(ws, ws_bytes, where, dev),
+                                 s), where)
 
 
 def _cache_rows(fn, where, c, k, v, seqs, start, counts, layer, stream):
@@ -692,8 +701,8 @@ def cb_cache_attend(c: cb_cache, q, out, ws=None, lse=None, seqs=None, q_lens=No
     _check(_lib.cb_cache_attend(_byref(c), layer, shape[0], _ints(seqs, where, dev, n), n,
                                 q.data_ptr(), _S4(*qs), shape[2], _ints(q_lens, where, dev, n),
                                 shape[3], causal, scale, out.data_ptr(), _S4(*os_),
-                                None if lse is None else lse.data_ptr(), kind, _ptr(ws),
-                                _nbytes(ws, ws_bytes), s), where)
+                                None if lse is None else lse.data_ptr(), kind,
+                                *_scratch(ws, ws_bytes, where, dev), s), where)
 
 
 __all__ = ["cb_layout", "layout", "layout_of", "cb_score_workspace_bytes", "cb_score",

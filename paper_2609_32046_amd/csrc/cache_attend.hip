@@ -85,8 +85,19 @@ __device__ inline int seq_len(const AttendArgs& a, int b) {
   return len < 0 ? 0 : (int64_t)len < room ? len : (int)room;
 }
 
+// The same through the scalar cache, for a row that the whole wave asks for.
+__device__ inline int seq_of(const AttendArgs& a, int b) {
+  return a.seqs ? ((ConstInts)a.seqs)[b] : b;
+}
+__device__ inline int uniform_len(const AttendArgs& a, int b) {
+  const int s = seq_of(a, b);
+  if ((unsigned)s >= (unsigned)a.c.seqs) return 0;
+  const int len = ((ConstInts)a.c.lens)[s];
+  const int64_t room = (int64_t)a.c.width << a.c.page_shift;
+  return len < 0 ? 0 : (int64_t)len < room ? len : (int)room;
+}
 __device__ inline int query_tokens(const AttendArgs& a, int b) {
-  const int m = a.q_lens ? a.q_lens[b] : (int)a.q_len;
+  const int m = a.q_lens ? ((ConstInts)a.q_lens)[b] : (int)a.q_len;
   return m < 0 ? 0 : m < (int)a.q_len ? m : (int)a.q_len;
 }
 
@@ -116,7 +127,7 @@ struct Run {
 __device__ inline int64_t rounds_per_run(const AttendArgs& a, int64_t* total) {
   int64_t t = 0;
   if (a.n == 1) {
-    t = rounds_of(seq_len(a, 0));
+    t = rounds_of(uniform_len(a, 0));
   } else {
     for (int i = threadIdx.x & 63; i < a.n; i += 64) t += rounds_of(seq_len(a, i));
     t = wave_sum64(t);
@@ -320,12 +331,12 @@ __global__ __launch_bounds__(kThreads, RT == 1 && !F32 ? 3 : 2) void attend_kern
   // The run's sequences, one after the other.
   for (; run.b < a.n && run.before < run.hi; ++run.b) {
     const int b = run.b;
-    const int seq = uniform(a.seqs ? a.seqs[b] : b);
-    const int len = uniform(seq_len(a, b));
+    const int seq = seq_of(a, b);
+    const int len = uniform_len(a, b);
     const int64_t before = run.before;
     const int rounds = rounds_of(len);
     run.before += rounds;
-    const int m = uniform(query_tokens(a, b));
+    const int m = query_tokens(a, b);
     const int rows = m * G;   // at most 2^26
     if (row0 >= rows) continue;   // also m = 0; uniform over the workgroup
     const int rlo = (int)(run.lo > before ? run.lo - before : 0);
@@ -659,7 +670,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, uint32_t
     before = uniform64(wave_sum64(before));
   }
   const int64_t first = before / per;
-  const int count = (int)((before + rounds_of(seq_len(a, b)) - 1) / per - first) + 1;
+  const int count = (int)((before + rounds_of(uniform_len(a, b)) - 1) / per - first) + 1;
   if (count == 1 || !live) return;
   const int d0 = ((int)threadIdx.x % kLanes) * 4;
   const int64_t base = ((int64_t)layer * a.c.heads + head) * a.slots + first + b;
@@ -761,15 +772,17 @@ bool make_attend_plan(int layers, int n, int heads, int q_heads, int64_t q_len, 
                       int64_t capacity, AttendPlan* p) {
   const int64_t rows = q_len * (q_heads / heads);
   if (rows > (1 << 26)) return false;
-  // blocks of a wave share a step's conversions; with fp32 rows two do not fit the
-  // registers at D = 128
-  p->blocks = rows <= 16 || (f32 && D == 128) ? 1 : rows <= 32 || f32 ? 2 : 4;
+  // no run shorter than kShortest rounds even where every sequence is full
+  const int64_t most = (int64_t)n * ((capacity + kShortest * kRound - 1) / (kShortest * kRound));
+  // Blocks of a wave share a step's conversions; with fp32 rows two do not fit the
+  // registers at D = 128.  A call that cannot fill the device takes one block to a wave: more
+  // workgroups, each sooner done (32 fp32 rows over 512 positions: 7.2 us, 10.3 with two).
+  const int64_t single = (rows + 15) / 16 * heads * layers;
+  p->blocks = rows <= 16 || (f32 && D == 128) || single * most <= kUnits ? 1 : rows <= 32 || f32 ? 2 : 4;
   const int64_t per = p->blocks * 16;
   const int64_t tiles = (rows + per - 1) / per;
   const int64_t sets = tiles * heads * layers;
   const int64_t resident = kUnits * (p->blocks == 1 ? 3 : 2);
-  // no run shorter than kShortest rounds even where every sequence is full
-  const int64_t most = (int64_t)n * ((capacity + kShortest * kRound - 1) / (kShortest * kRound));
   // Workgroups run in rounds of `resident`: the number of runs that leaves least of the last
   // one idle, the pieces of a further run counting for a fiftieth.
   int64_t target = 1;

@@ -693,6 +693,79 @@ def test_calls_refuse_tensors(torch, cb):
 # ---- all of it together -----------------------------------------------------------
 
 
+def test_a_round_of_answers_in_a_graph(torch, cb):
+    """Free, fork, extend, rotate, write, attend and thin, captured once and replayed on inputs that change, with eager
+    work and synchronisation between: every replay as the same calls run eagerly on a second cache."""
+    D, P, Hkv, G, kids = 64, 16, 2, 2, 3
+    lens = [203, 0, 0, 0, 0]
+    a, b = (cache_with(torch, cb, lens, H=Hkv, D=D, P=P, extra=40, width=15, seed=5) for _ in range(2))
+    for c in (a, b):
+        fill_cache(torch, cb, c, lens, 6)
+    par, chi, one, thin = ints(torch, [0] * kids), ints(torch, [1, 2, 3]), ints(torch, [1] * kids), ints(torch, [4])
+    src = ints(torch, [2])
+    freq = torch.tensor(cb.cb_rotary_frequencies(D, 1e4)[0], dtype=torch.float64, device="cuda")
+    k, v = (torch.empty((1, kids, Hkv, 1, D), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    q = torch.empty((1, kids, Hkv * G, 1, D), dtype=torch.bfloat16, device="cuda")
+    idx = torch.empty((1, 1, 1, 50), dtype=torch.int32, device="cuda")
+    pos = ints(torch, [203])
+
+    def scratches(c):
+        return [torch.empty(n, dtype=torch.uint8, device="cuda") for n in (
+            cb.cb_cache_fork_workspace_bytes(c.desc, kids), cb.cb_cache_compact_workspace_bytes(c.desc, 1))]
+
+    def step(c, ws, kk, qq, out, lse, aw):
+        cb.cb_cache_free(c.desc, chi)
+        cb.cb_cache_fork(c.desc, par, chi, c.status, ws[0])
+        cb.cb_cache_extend(c.desc, chi, one, c.status)
+        cb.cb_rotary([cb.rows(q[0], qq[0], pos), cb.rows(k[0], kk[0], pos)], freq)
+        cb.cb_cache_write(c.desc, kk, v, chi)
+        cb.cb_cache_attend(c.desc, qq, out, aw, lse, chi)
+        cb.cb_cache_compact(c.desc, src, thin, idx, c.status, ws[1])
+
+    def fresh(i):
+        for x, n in ((k, 0), (v, 1), (q, 2)):
+            x.copy_(randn(torch, 100 + 10 * i + n, *x.shape))
+        idx.copy_(torch.sort(torch.randperm(204, generator=torch.Generator().manual_seed(i))[:50])[0].reshape(1, 1, 1, 50))
+
+    bufs = []
+    for c in (a, b):
+        qq = torch.empty_like(q)
+        bufs.append((scratches(c), torch.empty_like(k), qq, torch.empty_like(q),
+                     torch.empty(q.shape[:4], device="cuda"), scratch(torch, cb, c, q)))
+    fresh(0)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(a, *bufs[0])
+    torch.cuda.current_stream().wait_stream(side)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step(a, *bufs[0])
+    step(b, *bufs[1])
+    for i in range(4):
+        fresh(i)
+        bufs[0][3].zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        step(b, *bufs[1])
+        assert a.status.item() == b.status.item() == 0
+        for x, y in ((a.pool, b.pool), (a.refs, b.refs), (a.table, b.table), (a.lens, b.lens),
+                     (bufs[0][3], bufs[1][3]), (bufs[0][4], bufs[1][4])):
+            assert torch.equal(x, y)
+        m = model(a, D, P)
+        check_attend(torch, m, bufs[0][2], bufs[0][3], bufs[0][4], [1, 2, 3], [1] * kids, True, 0.0, 0, "bf16")
+        assert m.lens.tolist() == [203, 204, 204, 204, 50]
+
+
+def test_scratch_on_the_wrong_device_is_refused(torch, cb):
+    c = cache_with(torch, cb, [20], D=64, P=16)
+    one, ws = ints(torch, [0]), torch.empty(1 << 16, dtype=torch.uint8)
+    with pytest.raises(cb.CBError):
+        cb.cb_cache_fork(c.desc, one, one, c.status, ws)
+    with pytest.raises(cb.CBError):
+        cb.cb_cache_fork(c.desc, one, one, c.status, ws[::2].cuda()[::2])
+
+
 def test_a_message_from_selection_to_answers(torch, cb, oracle):
     """The receiver's path: select and compact two senders' caches, move the kept keys, store them, fork two
     answers, append a token to each, attend, thin one answer, attend again."""
