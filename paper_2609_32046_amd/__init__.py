@@ -404,13 +404,17 @@ class PositionBuffers:
 _S3, _S4 = _i64 * 3, _i64 * 4
 _byref = ctypes.byref
 _torch = None
+_raw_stream = None
 
 
 def _lazy_torch():
-    global _torch
+    global _torch, _raw_stream
     if _torch is None:
         import torch
 
+        # the current stream's handle without a Stream object (a microsecond a call)
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+            lambda dev: torch.cuda.current_stream(dev).cuda_stream)
         _torch = torch
     return _torch
 
@@ -421,7 +425,7 @@ def _now(stream):
     torch = _torch or _lazy_torch()
     dev = torch.cuda.current_device()
     if stream is None:
-        return dev, torch.cuda.current_stream(dev).cuda_stream
+        return dev, _raw_stream(dev)
     return dev, stream if isinstance(stream, int) else stream.cuda_stream
 
 

@@ -88,21 +88,31 @@ struct PlanShared {
   int offset[kCacheMaxEntries + 1];   // pages that the entries before need
 };
 
-// Fills a list (a barrier follows); entries outside the table get no pages.  Returns
-// whether one of this thread's is outside.
-__device__ inline bool fill_list(const CacheView& c, SeqList& l, const int32_t* seqs, int n) {
+// Fills N lists (a barrier follows), their reads side by side; entries outside the table get no
+// pages.  Returns whether one of this thread's is outside.
+template <int N>
+__device__ inline bool fill_lists(const CacheView& c, SeqList* const (&l)[N],
+                                  const int32_t* const (&seqs)[N], int n) {
   bool bad = false;
-  int most = 0;
+  int most[N] = {};
   for (int i = threadIdx.x; i < n; i += kPlan) {
-    const int s = seqs[i];
-    const int len = known(c, s) ? c.lens[s] : 0;
-    bad |= !known(c, s) || len < 0;
-    l.seq[i] = s;
-    l.len[i] = len;
-    const int k = held_pages(c, len);
-    most = k > most ? k : most;
+    int s[N], len[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) s[k] = seqs[k][i];
+#pragma unroll
+    for (int k = 0; k < N; ++k) len[k] = known(c, s[k]) ? c.lens[s[k]] : 0;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      bad |= !known(c, s[k]) || len[k] < 0;
+      l[k]->seq[i] = s[k];
+      l[k]->len[i] = len[k];
+      const int p = held_pages(c, len[k]);
+      most[k] = p > most[k] ? p : most[k];
+    }
   }
-  if (most > 0) atomicMax(&l.most, most);
+#pragma unroll
+  for (int k = 0; k < N; ++k)
+    if (most[k] > 0) atomicMax(&l[k]->most, most[k]);
   return bad;
 }
 
@@ -243,10 +253,13 @@ __global__ __launch_bounds__(kPlan) void cache_extend_kernel(CacheView c,
   if (threadIdx.x == 0) sh.bad = l.most = 0;
   __syncthreads();
   const int64_t room = (int64_t)c.width << c.page_shift;
-  bool bad = fill_list(c, l, seqs, n);
-  for (int i = threadIdx.x; i < n; i += kPlan)   // this thread's own entries
-    bad |= (known(c, l.seq[i]) && mark(bits, l.seq[i])) || add[i] < 0 ||
-           (int64_t)l.len[i] + add[i] > room;
+  const int mine = (int)threadIdx.x < n ? add[threadIdx.x] : 0;   // under way beside the lists
+  bool bad = fill_lists<1>(c, {&l}, {seqs}, n);
+  for (int i = threadIdx.x; i < n; i += kPlan) {   // this thread's own entries
+    const int more = i < kPlan ? mine : add[i];
+    bad |= (known(c, l.seq[i]) && mark(bits, l.seq[i])) || more < 0 ||
+           (int64_t)l.len[i] + more > room;
+  }
   if (bad) sh.bad = 1;
   __syncthreads();
   if (sh.bad) {
@@ -254,7 +267,9 @@ __global__ __launch_bounds__(kPlan) void cache_extend_kernel(CacheView c,
     return;
   }
   const int64_t want = plan_offsets(
-      sh, n, [&](int i) { return held_pages(c, l.len[i] + add[i]) - held_pages(c, l.len[i]); });
+      sh, n, [&](int i) {   // every thread asks for its own entries
+        return held_pages(c, l.len[i] + (i < kPlan ? mine : add[i])) - held_pages(c, l.len[i]);
+      });
   const int64_t have = take_free(c, sh, want, [&](int page, int rank) {
     const int i = entry_of(sh, n, rank);
     c.table[(int64_t)l.seq[i] * c.width + held_pages(c, l.len[i]) + rank - sh.offset[i]] = page;
@@ -264,7 +279,8 @@ __global__ __launch_bounds__(kPlan) void cache_extend_kernel(CacheView c,
     if (threadIdx.x == 0) *status = lacking(want - have);
     return;
   }
-  for (int i = threadIdx.x; i < n; i += kPlan) c.lens[l.seq[i]] = l.len[i] + add[i];
+  for (int i = threadIdx.x; i < n; i += kPlan)
+    c.lens[l.seq[i]] = l.len[i] + (i < kPlan ? mine : add[i]);
   if (threadIdx.x == 0) *status = 0;
 }
 
@@ -327,8 +343,7 @@ __global__ __launch_bounds__(kPlan) void cache_fork_kernel(CacheView c,
     *count = 0;
   }
   __syncthreads();
-  bool bad = fill_list(c, from, parents, n);
-  bad |= fill_list(c, to, children, n);
+  bool bad = fill_lists<2>(c, {&from, &to}, {parents, children}, n);
   for (int i = threadIdx.x; i < n; i += kPlan)   // this thread's own entries
     bad |= known(c, to.seq[i]) && mark(bits, to.seq[i]);
   if (bad) sh.bad = 1;
@@ -432,8 +447,7 @@ __global__ __launch_bounds__(kPlan) void cache_compact_plan_kernel(CacheCompactA
   clear_bits(bits, c.seqs);
   if (threadIdx.x == 0) sh.bad = from.most = to.most = 0;
   __syncthreads();
-  bool bad = fill_list(c, from, a.src, n);
-  bad |= fill_list(c, to, a.dst, n);
+  bool bad = fill_lists<2>(c, {&from, &to}, {a.src, a.dst}, n);
   for (int i = threadIdx.x; i < n; i += kPlan) {   // this thread's own entries
     const int64_t k = kept(a, i);
     bad |= k < 0 || k > a.keep || (known(c, to.seq[i]) && mark(bits, to.seq[i]));
