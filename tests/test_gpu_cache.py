@@ -527,7 +527,8 @@ def test_attend_single_tokens(torch, cb, dtype, D, P, Hkv, G):
 
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("D,P,G,m", [(128, 32, 4, 5), (64, 16, 3, 7), (128, 16, 1, 33), (64, 64, 8, 20), (128, 128, 5, 50)])
+@pytest.mark.parametrize("D,P,G,m", [(128, 32, 4, 5), (64, 16, 3, 7), (128, 16, 1, 33), (64, 64, 8, 20), (128, 128, 5, 50),
+                                       (64, 16, 7, 40), (128, 32, 8, 65)])
 def test_attend_several_tokens(torch, cb, causal, dtype, D, P, G, m):
     """Prompts' parts: more query tokens than positions (rows of no position), ragged query counts, one
     of none, sequences named out of order and twice, the second layer."""
@@ -542,6 +543,8 @@ def test_attend_long_sequences_in_chunks(torch, cb, dtype):
     attend_case(torch, cb, [5000, 0, 1, 700, 2049], 1, 4, 128, 64, 1, dtype, True, seed=3)
     attend_case(torch, cb, [3001, 1300], 1, 6, 64, 16, 7, dtype, True, seed=4)
     attend_case(torch, cb, [2600], 2, 2, 128, 32, 3, dtype, False, layers=2, seed=5)
+    attend_case(torch, cb, [2100, 0, 900], 1, 4, 128, 64, 60, dtype, True, seed=16)
+    attend_case(torch, cb, [2100, 300], 1, 5, 64, 16, 50, dtype, False, seed=17, holes=[(0, 3), (0, 130), (1, 0)])
 
 
 def test_attend_many_sequences(torch, cb):
@@ -559,8 +562,8 @@ def test_attend_scale_and_large_logits(torch, cb):
     attend_case(torch, cb, [100, 400], 1, 2, 128, 16, 3, "bf16", True, scale=1e-30, seed=10)
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_attend_masked_places_hold_anything(torch, cb, dtype):
+@pytest.mark.parametrize("dtype,G", [("bf16", 3), ("f32", 3), ("bf16", 20), ("bf16", 30)])
+def test_attend_masked_places_hold_anything(torch, cb, dtype, G):
     """Positions behind the limit with NaN groups, infinite values and any bytes: rows that do not see
     them stay as they are, rows that do are NaN in the group's values (or wholly, for a key)."""
     D, P, lens, m = 128, 32, [75, 40], 12
@@ -580,14 +583,15 @@ def test_attend_masked_places_hold_anything(torch, cb, dtype):
         q = 38 - 32
         c.pool[int(pages[1, 1]), 0, :, 2 * n + q * 4 + 2] = 255
 
-    _, _, out, _, _ = attend_case(torch, cb, lens, 1, 3, D, P, m, dtype, True, seed=11, prepare=spoil)
+    _, _, out, _, _ = attend_case(torch, cb, lens, 1, G, D, P, m, dtype, True, seed=11, prepare=spoil)
     nan = torch.isnan(out[0, 0])                  # [heads][rows][D]
     assert nan[:, 7:, 32:64].all() and not nan[:, :7].any() and not nan[:, 7:, :32].any()
     nan = torch.isnan(out[0, 1])
     assert nan[:, 10:].all() and not nan[:, :10].any()
 
 
-def test_attend_nan_in_the_open(torch, cb):
+@pytest.mark.parametrize("dtype,m", [("f32", 1), ("bf16", 1), ("bf16", 110)])
+def test_attend_nan_in_the_open(torch, cb, dtype, m):
     """A NaN value group far from any mask reaches every row, in its group only."""
     D, P = 64, 16
 
@@ -595,7 +599,7 @@ def test_attend_nan_in_the_open(torch, cb):
         n, s = P * D // 2, P * D // 32
         c.pool[int(c.table[0, 3]), 0, 0, 2 * n + s + (5 // 4 * 2 + 1) * 4 + 5 % 4] = 255
 
-    _, _, out, _, _ = attend_case(torch, cb, [1000], 1, 2, D, P, 1, "f32", True, seed=12, prepare=spoil)
+    _, _, out, _, _ = attend_case(torch, cb, [1000], 1, 2, D, P, m, dtype, True, seed=12, prepare=spoil)
     assert torch.isnan(out[..., 32:]).all() and not torch.isnan(out[..., :32]).any()
 
 
