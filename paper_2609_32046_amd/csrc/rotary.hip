@@ -15,6 +15,11 @@ constexpr int kThreads = 256;
 constexpr int kHeads = 4;   // rows of one position that a thread turns by the same angles
 constexpr int64_t kStreamBytes = (int64_t)256 << 20;
 
+// A piece of a row: mode 0, half layout with halves of whole vectors of eight: eight pairs
+// from both halves, then copied vectors; 1, interleaved: eight consecutive values; 2, half
+// layout with other halves: up to eight pairs, the upper ones from anywhere, then up to
+// eight copied values.
+//
 // 16 bytes; STREAM: past the caches, for calls that would only flush them.
 template <bool STREAM, typename V, typename T>
 __device__ inline V get16(const T* p) {
@@ -33,6 +38,8 @@ struct Vec8;
 template <>
 struct Vec8<float> {
   f32x4 a, b;
+  __device__ void load_any(const float* p) { __builtin_memcpy(this, p, sizeof *this); }
+  __device__ void store_any(float* p) const { __builtin_memcpy(p, this, sizeof *this); }
   template <bool S>
   __device__ void load(const float* p) {
     a = get16<S, f32x4>(p);
@@ -52,6 +59,8 @@ struct Vec8<float> {
 template <>
 struct Vec8<__bf16> {
   u32x4 a;
+  __device__ void load_any(const __bf16* p) { __builtin_memcpy(this, p, sizeof *this); }
+  __device__ void store_any(__bf16* p) const { __builtin_memcpy(p, this, sizeof *this); }
   template <bool S>
   __device__ void load(const __bf16* p) { a = get16<S, u32x4>(p); }
   template <bool S>
@@ -85,13 +94,9 @@ __device__ inline void angle(double delta, double freq, float amplitude, float s
   *sn = __builtin_amdgcn_sinf(r) * (amplitude * sign);
 }
 
-// Kind of a work item's chunk of a row: 0, half layout in 16-byte vectors: eight pairs
-// from both halves, then copied vectors of eight; 1, interleaved: eight consecutive
-// values; 2, half layout with halves that are no multiple of eight: one pair,
-// then single copied values.
 template <typename T, int MODE, bool STREAM>
 struct Turn {
-  static constexpr int PAIRS = MODE == 0 ? 8 : MODE == 1 ? 4 : 1;
+  static constexpr int PAIRS = MODE == 1 ? 4 : 8;
 
   // N rows of consecutive heads, chunk ch.  No branch between the loads: the rows, the positions
   // and the frequencies are all under way together.
@@ -99,8 +104,11 @@ struct Turn {
   __device__ static void rows(const RotaryArgs& a, const RotaryPart& p, const T* in, T* out,
                               const int32_t* pos, const int32_t* from, int ch) {
     const int half = a.R / 2;
-    Vec8<T> lo[MODE == 2 ? 1 : N], hi[MODE == 0 ? N : 1];
-    float l1[MODE == 2 ? N : 1], h1[MODE == 2 ? N : 1];
+    Vec8<T> lo[N], hi[MODE == 1 ? 1 : N];
+    // mode 2: pairs of this piece; the last one, of fewer than eight, begins earlier so that it reads
+    // eight too, and keeps those of its own
+    const int some = half - ch * 8;
+    const int base = MODE == 2 && some < 8 && half >= 8 ? half - 8 : ch * PAIRS;
     int64_t to[N], old[N];
     double freq[PAIRS];
 #pragma unroll
@@ -111,9 +119,17 @@ struct Turn {
         hi[h].template load<STREAM>(r + half + ch * 8);
       } else if constexpr (MODE == 1) {
         lo[h].template load<STREAM>(r + ch * 8);
+      } else if (half >= 8) {
+        lo[h].load_any(r + base);
+        hi[h].load_any(r + half + base);
       } else {
-        l1[h] = load1(r + ch);
-        h1[h] = load1(r + half + ch);
+        float u[8] = {}, v[8] = {};
+        for (int i = 0; i < half; ++i) {
+          u[i] = load1(r + i);
+          v[i] = load1(r + half + i);
+        }
+        lo[h].set(u);   // exact: the values are of this type
+        hi[h].set(v);
       }
     }
 #pragma unroll
@@ -127,8 +143,8 @@ struct Turn {
     }
 #pragma unroll
     for (int i = 0; i < PAIRS; ++i) {
-      const int pair = ch * PAIRS + i;
-      freq[i] = a.freq[MODE == 1 && pair >= half ? half - 1 : pair];
+      const int pair = base + i;
+      freq[i] = a.freq[MODE != 0 && pair >= half ? half - 1 : pair];
     }
     const bool shared = p.pos_stride[1] == 0 && (!from || p.from_stride[1] == 0);
     float cs[PAIRS], sn[PAIRS];
@@ -141,7 +157,7 @@ struct Turn {
           angle(delta, freq[i], a.amplitude, a.sign, &cs[i], &sn[i]);
       }
       T* w = out + h * p.out_stride[1];
-      if constexpr (MODE == 0) {
+      if constexpr (MODE != 1) {
         float u[8], v[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -151,9 +167,21 @@ struct Turn {
         }
         lo[h].set(u);
         hi[h].set(v);
-        lo[h].template store<STREAM>(w + ch * 8);
-        hi[h].template store<STREAM>(w + half + ch * 8);
-      } else if constexpr (MODE == 1) {
+        if (MODE == 0) {
+          lo[h].template store<STREAM>(w + ch * 8);
+          hi[h].template store<STREAM>(w + half + ch * 8);
+        } else if (some >= 8) {
+          lo[h].template store<STREAM>(w + ch * 8);
+          hi[h].store_any(w + half + ch * 8);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (base + i >= ch * 8 && base + i < half) {
+              w[base + i] = (T)u[i];
+              w[half + base + i] = (T)v[i];
+            }
+        }
+      } else {
         float u[8];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -164,9 +192,6 @@ struct Turn {
         }
         lo[h].set(u);
         lo[h].template store<STREAM>(w + ch * 8);
-      } else {
-        w[ch] = (T)(l1[h] * cs[0] - h1[h] * sn[0]);
-        w[half + ch] = (T)(h1[h] * cs[0] + l1[h] * sn[0]);
       }
     }
   }
@@ -176,8 +201,8 @@ template <typename T, int MODE, bool STREAM>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a) {
   const RotaryPart& p = a.part[blockIdx.z];
   const int half = a.R / 2;
-  const int turned = MODE == 0 ? half / 8 : MODE == 1 ? a.D / 8 : half;
-  const int copied = MODE == 0 ? (a.D - a.R) / 8 : MODE == 1 ? 0 : a.D - a.R;
+  const int turned = MODE == 1 ? a.D / 8 : (half + 7) / 8;
+  const int copied = MODE == 1 ? 0 : (a.D - a.R + 7) / 8;
   const int chunks = turned + copied;
   const int64_t items = p.size[2] * chunks;
   const int64_t head_blocks = (p.size[1] + kHeads - 1) / kHeads;
@@ -202,13 +227,18 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a) {
                                  : nullptr;
     if (ch >= turned) {   // behind the rotated values
       for (int h = 0; h < nh; ++h) {
-        const int at = MODE == 0 ? a.R + (ch - turned) * 8 : a.R + (ch - turned);
-        if constexpr (MODE == 0) {
-          Vec8<T> x;
-          x.template load<STREAM>(in + h * p.in_stride[1] + at);
-          x.template store<STREAM>(out + h * p.out_stride[1] + at);
+        const int at = a.R + (ch - turned) * 8;
+        const T* from_row = in + h * p.in_stride[1] + at;
+        T* to_row = out + h * p.out_stride[1] + at;
+        Vec8<T> x;
+        if (MODE == 0) {
+          x.template load<STREAM>(from_row);
+          x.template store<STREAM>(to_row);
+        } else if (at + 8 <= a.D) {
+          x.load_any(from_row);
+          x.store_any(to_row);
         } else {
-          out[h * p.out_stride[1] + at] = in[h * p.in_stride[1] + at];
+          for (int i = 0; i < 8 && at + i < a.D; ++i) to_row[i] = from_row[i];
         }
       }
     } else if (nh == kHeads) {
@@ -235,8 +265,7 @@ hipError_t launch_rotary(const RotaryArgs& a, int parts, bool interleaved, bool 
                          hipStream_t s) {
   const int half = a.R / 2;
   const int mode = interleaved ? 1 : half % 8 == 0 ? 0 : 2;
-  const int chunks = mode == 0 ? half / 8 + (a.D - a.R) / 8 : mode == 1 ? a.D / 8
-                                                                       : half + a.D - a.R;
+  const int chunks = mode == 1 ? a.D / 8 : (half + 7) / 8 + (a.D - a.R + 7) / 8;
   int64_t gx = 0, gy = 0, values = 0;
   for (int i = 0; i < parts; ++i) {
     const RotaryPart& p = a.part[i];

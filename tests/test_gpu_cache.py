@@ -76,6 +76,9 @@ def test_rotary(torch, cb, dtype, interleaved, D, R):
     for transpose in (False, True):
         qo, ko = torch.full_like(q, 7.0), torch.full_like(k, 7.0)
         cb.cb_rotary([cb.rows(q, qo, pos), cb.rows(k, ko, pos)], fd, amp, interleaved, transpose)
+        qi, ki = q.clone(), k.clone()   # in place: the same bits
+        cb.cb_rotary([cb.rows(qi, qi, pos), cb.rows(ki, ki, pos)], fd, amp, interleaved, transpose)
+        assert torch.equal(qi, qo) and torch.equal(ki, ko)
         for x, y in ((q, qo), (k, ko)):
             d = pos.cpu().numpy().astype(np.float64) * np.ones((2, x.shape[1], 7))
             check_rotary(torch, y, x, freq, d, amp, interleaved, transpose, dtype)
