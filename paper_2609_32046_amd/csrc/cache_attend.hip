@@ -767,8 +767,12 @@ hipError_t launch(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
 // Workgroups resident at a time: 256 compute units, three each of the
 // 16-row kernels, two of the others.
 constexpr int64_t kUnits = 256;
-// Rounds of the shortest run: joining costs a launch, about as long as eight rounds take.
-constexpr int64_t kShortest = 4;
+// Rounds of the shortest run: 16 sequences of 1024 positions take 16.3 us in runs of two
+// rounds, 18.4 of four, 21.8 of eight.
+constexpr int64_t kShortest = 2;
+// One sequence of up to so many rounds stays whole, and nothing is joined: 1024 positions take
+// 11.3 us so and 14.6 cut, 2048 positions 15.0 with runs that long and 13.5 with short ones.
+constexpr int64_t kWhole = 8;
 
 bool make_attend_plan(int layers, int n, int heads, int q_heads, int64_t q_len, int D, bool f32,
                       int64_t capacity, AttendPlan* p) {
@@ -799,6 +803,7 @@ bool make_attend_plan(int layers, int n, int heads, int q_heads, int64_t q_len, 
     }
   }
   if (target > most) target = most;
+  if (n == 1 && capacity <= kWhole * kRound) target = 1;
   p->row_tiles = (int32_t)tiles;
   p->rows_pad = (int32_t)(tiles * per);
   p->target = (int32_t)target;
