@@ -28,35 +28,30 @@ __device__ inline bool known(const CacheView& c, int seq) {
   return (unsigned)seq < (unsigned)c.seqs;
 }
 
-__device__ inline int wave_sum(int x) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) x += __shfl_xor(x, d);
-  return x;
-}
-
 // Inclusive sum over the lanes up to this one.
-__device__ inline int wave_scan(int x) {
+template <typename I>
+__device__ inline I wave_scan(I x) {
   const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
-    const int y = __shfl_up(x, d);
+    const I y = __shfl_up(x, d);
     if (lane >= d) x += y;
   }
   return x;
 }
 
-// Exclusive prefix of x over the workgroup, and the total.  `sums`: kPlanWaves
-// words; two barriers.
-__device__ inline int group_scan(int x, int* sums, int* total) {
+// Exclusive prefix of x over the workgroup, and the total, in 64 bits: the rows of a thousand
+// sequences can hold more than 2^31 pages.  `sums`: kPlanWaves words; two barriers.
+__device__ inline int64_t group_scan(int64_t x, int64_t* sums, int64_t* total) {
   const int wave = threadIdx.x >> 6;
-  const int incl = wave_scan(x);
+  const int64_t incl = wave_scan(x);
   __syncthreads();
   if ((threadIdx.x & 63) == 63) sums[wave] = incl;
   __syncthreads();
-  int before = 0, all = 0;
+  int64_t before = 0, all = 0;
 #pragma unroll
   for (int w = 0; w < kPlanWaves; ++w) {
-    const int v = sums[w];
+    const int64_t v = sums[w];
     before += w < wave ? v : 0;
     all += v;
   }
@@ -81,7 +76,7 @@ struct SeqList {
 };
 
 struct PlanShared {
-  int sums[kPlanWaves];
+  int64_t sums[kPlanWaves];
   int rows[kScan * kPlanWaves];
   int free;
   int bad;
@@ -127,9 +122,8 @@ __device__ inline int64_t plan_offsets(PlanShared& sh, int n, Need need) {
   int64_t base = 0;
   for (int i0 = 0; i0 < n; i0 += kPlan) {
     const int i = i0 + threadIdx.x;
-    int total;
-    const int before = group_scan(i < n ? need(i) : 0, sh.sums, &total);
-    const int64_t at = base + before;
+    int64_t total;
+    const int64_t at = base + group_scan(i < n ? need(i) : 0, sh.sums, &total);
     if (i < n) sh.offset[i] = at > kCacheMaxPages ? kCacheMaxPages + 1 : (int)at;
     base += total;
   }

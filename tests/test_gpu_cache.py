@@ -335,6 +335,20 @@ def test_extend(torch, cb):
         same_state(c, m)
 
 
+def test_needs_of_more_than_32_bits(torch, cb):
+    """A thousand rows of two million pages: what they ask for together passes 2^31 pages."""
+    n, width, P = 1024, 1 << 21, 16
+    c = cb.Cache(1, 1, 64, P, 64, n, width)
+    seqs = torch.arange(n, dtype=torch.int32, device="cuda")
+    cb.cb_cache_extend(c.desc, seqs, torch.full((n,), width * P, dtype=torch.int32, device="cuda"), c.status)
+    assert c.status.item() == n * width - 64
+    idx = torch.zeros(width * P, dtype=torch.int32, device="cuda").expand(n, 1, 1, width * P)
+    ws = torch.empty(cb.cb_cache_compact_workspace_bytes(c.desc, n), dtype=torch.uint8, device="cuda")
+    cb.cb_cache_compact(c.desc, seqs, seqs, idx, c.status, ws)
+    assert c.status.item() == n * width - 64
+    assert not c.lens.any() and not c.refs.any() and int(c.table.max()) == -1
+
+
 def test_free(torch, cb):
     """Shared pages stay with their other holders; repeated and unknown entries pass."""
     D, P = 64, 16
