@@ -18,7 +18,10 @@
  * Strided tensors: row strides are given in elements, outermost first; the D
  * values of a row are contiguous, and every row starts on a 16-byte boundary
  * (pointers and strides; CB_ERR_ALIGN otherwise).  A size of zero launches
- * nothing.  Outputs must not overlap inputs unless a call says so.
+ * nothing.  Outputs must not overlap inputs unless a call says so.  Sizes that pass
+ * the limits named at a call, or one launch's (2^32 - 1 threads along an axis: eight
+ * values a thread for rows, 16 to 64 query rows a workgroup for attention), give
+ * CB_ERR_SHAPE.
  */
 #ifndef CACHEBACK_CACHE_H
 #define CACHEBACK_CACHE_H
@@ -142,7 +145,7 @@ int cb_cache_extend(const cb_cache* c, const int32_t* seqs, const int32_t* add, 
 
 /* Gives back the pages of the sequences: their lengths become 0 and their
  * table rows -1.  Entries outside the table are passed over, and so is an
- * entry listed again. */
+ * entry listed again.  n < 2^24. */
 int cb_cache_free(const cb_cache* c, const int32_t* seqs, int32_t n, void* stream);
 
 /* children[i] becomes a sequence with the positions of parents[i]: it holds

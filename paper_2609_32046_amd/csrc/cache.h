@@ -9,6 +9,7 @@ namespace cb {
 constexpr int kCacheMaxEntries = 2048;     // entries of a page call: their lists lie in LDS
 constexpr int kCacheMaxSeqs = 1 << 17;     // its bit set of sequences fills 16 KiB of LDS
 constexpr int kCacheMaxPages = 1 << 24;
+constexpr int64_t kMaxThreads = 0xffffffff;   // of a grid, along one axis
 
 // The cache as kernels see it.
 struct CacheView {

@@ -87,9 +87,10 @@ int rows_args(const cb_cache* c, int32_t layer0, int32_t layers, const int32_t* 
   const int64_t size[4] = {layers, n, c->kv_heads, max_count};
   st = check_strides(stride, size, 4, dtype == CB_F32 ? 4 : 2, output);
   if (st != CB_OK) return st;
-  // blocks of 256 threads, eight values a thread, in a grid of at most 2^31 - 1
+  // a thread for eight values
   const int64_t units = (int64_t)layers * n * c->kv_heads;
-  if (units > 0 && max_count > ((int64_t)0x7fffffff * 16) / units) return CB_ERR_SHAPE;
+  if (units > 0 && max_count > (cb::kMaxThreads - 255) / (c->head_dim / 8) / units)
+    return CB_ERR_SHAPE;
   a->k = k;
   a->v = v;
   a->seqs = seqs;
@@ -166,8 +167,8 @@ int cb_rotary(const cb_rows* rows, int32_t parts, int32_t head_dim, const double
       total *= r.size[d] ? r.size[d] : 1;
       if (total > ((int64_t)1 << 40)) return CB_ERR_SHAPE;
     }
-    // a grid of at most 2^31 - 1 workgroups along the rows of one head
-    if (r.size[2] * head_dim > (int64_t)0x7fffffff * 64) return CB_ERR_SHAPE;
+    // a thread for eight values of the rows of one head
+    if (r.size[2] > (cb::kMaxThreads - 255) / (head_dim / 8 + 1)) return CB_ERR_SHAPE;
     const bool none = r.size[0] == 0 || r.size[1] == 0 || r.size[2] == 0;
     if (!none && (!r.in || !r.out || !r.pos)) return CB_ERR_NULL;
     if (!aligned(r.in, 16) || !aligned(r.out, 16) || !aligned(r.pos, 4) || !aligned(r.from, 4))
@@ -228,7 +229,7 @@ int cb_cache_free(const cb_cache* c, const int32_t* seqs, int32_t n, void* strea
   cb::CacheView v;
   const int st = view_of(c, &v);
   if (st != CB_OK) return st;
-  if (n < 0) return CB_ERR_SHAPE;
+  if (n < 0 || n > cb::kMaxThreads / 256) return CB_ERR_SHAPE;
   if (n > 0 && !seqs) return CB_ERR_NULL;
   if (!aligned(seqs, 4)) return CB_ERR_ALIGN;
   return done(cb::launch_cache_free(v, seqs, n, static_cast<hipStream_t>(stream)));
@@ -346,7 +347,8 @@ int cb_cache_attend(const cb_cache* c, int32_t layer0, int32_t layers, const int
   st = attend_plan(c, layers, n, q_heads, q_len, dtype, &p);
   if (st != CB_OK) return st;
   if (!seqs && n > c->seqs) return CB_ERR_SHAPE;
-  if (!(scale >= 0.0) || !isfinite((float)scale)) return CB_ERR_SHAPE;
+  const double c2 = (scale == 0.0 ? 1.0 / sqrt((double)c->head_dim) : scale) * 1.4426950408889634;
+  if (!(scale >= 0.0) || !isfinite((float)c2)) return CB_ERR_SHAPE;
   const bool none = layers == 0 || n == 0 || q_len == 0;
   if (!q_stride || !out_stride || (!none && (!q || !out))) return CB_ERR_NULL;
   if (p.total > 0 && (!ws || ws_bytes < p.total)) return CB_ERR_WORKSPACE;
@@ -383,9 +385,7 @@ int cb_cache_attend(const cb_cache* c, int32_t layer0, int32_t layers, const int
   a.target = p.target;
   a.slots = p.slots;
   a.causal = causal != 0;
-  const double sc = scale == 0.0 ? 1.0 / sqrt((double)c->head_dim) : scale;
-  // never 0: a masked logit is -inf times it
-  a.c2 = fmaxf((float)(sc * 1.4426950408889634), 1e-37f);
+  a.c2 = fmaxf((float)c2, 1e-37f);   // never 0: a masked logit is -inf times it
   return done(cb::launch_cache_attend(a, p, dtype == CB_F32, static_cast<hipStream_t>(stream)));
 }
 

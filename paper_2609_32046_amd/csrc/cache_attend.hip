@@ -740,7 +740,7 @@ template <int D, bool F32>
 hipError_t launch(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
   constexpr int kMost = !F32 ? 4 : D == 64 ? 2 : 1;   // blocks of a wave, as in make_attend_plan
   const int64_t grid = (int64_t)a.c.heads * a.row_tiles * a.target * a.layers;
-  if (grid > 0x7fffffff) return hipErrorInvalidValue;
+  if (grid * kThreads > kMaxThreads) return hipErrorInvalidValue;
   if (p.blocks == 1) attend_kernel<D, F32, 1><<<(unsigned)grid, kThreads, 0, s>>>(a);
   else if (F32 || p.blocks == 2) attend_kernel<D, F32, kMost < 2 ? kMost : 2><<<(unsigned)grid, kThreads, 0, s>>>(a);
   else attend_kernel<D, F32, kMost><<<(unsigned)grid, kThreads, 0, s>>>(a);
@@ -754,7 +754,7 @@ hipError_t launch(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
   const bool many = a.target >= 8 * (int64_t)a.n && rows * a.c.heads * a.n * a.layers <= 4096;
   const int64_t blocks = many ? rows : (rows + kRows - 1) / kRows;
   const int64_t g2 = blocks * a.c.heads * a.n * a.layers;
-  if (g2 > 0x7fffffff) return hipErrorInvalidValue;
+  if (g2 * 256 > kMaxThreads) return hipErrorInvalidValue;
   if (many)
     attend_join_kernel<D, F32, kRows><<<(unsigned)g2, 256, 0, s>>>(a, (uint32_t)blocks);
   else
@@ -777,14 +777,16 @@ constexpr int64_t kWhole = 8;
 bool make_attend_plan(int layers, int n, int heads, int q_heads, int64_t q_len, int D, bool f32,
                       int64_t capacity, AttendPlan* p) {
   const int64_t rows = q_len * (q_heads / heads);
-  if (rows > (1 << 26)) return false;
+  const int64_t units = (int64_t)heads * layers * n;
+  if (rows > (1 << 26) || units > 0x7fffffff) return false;
   // no run shorter than kShortest rounds even where every sequence is full
   const int64_t most = (int64_t)n * ((capacity + kShortest * kRound - 1) / (kShortest * kRound));
   // Blocks of a wave share a step's conversions; with fp32 rows two do not fit the
   // registers at D = 128.  A call that cannot fill the device takes one block to a wave: more
   // workgroups, each sooner done (32 fp32 rows over 512 positions: 7.2 us, 10.3 with two).
   const int64_t single = (rows + 15) / 16 * heads * layers;
-  p->blocks = rows <= 16 || (f32 && D == 128) || single * most <= kUnits ? 1 : rows <= 32 || f32 ? 2 : 4;
+  p->blocks = rows <= 16 || (f32 && D == 128) || (single <= kUnits && single * most <= kUnits)
+                  ? 1 : rows <= 32 || f32 ? 2 : 4;
   const int64_t per = p->blocks * 16;
   const int64_t tiles = (rows + per - 1) / per;
   const int64_t sets = tiles * heads * layers;
@@ -808,7 +810,12 @@ bool make_attend_plan(int layers, int n, int heads, int q_heads, int64_t q_len, 
   p->rows_pad = (int32_t)(tiles * per);
   p->target = (int32_t)target;
   p->slots = (int32_t)(target + n);
-  if (sets * p->slots > 0x7fffffff || rows * heads * n * layers > 0x7fffffff) return false;
+  // threads of the two grids
+  const int64_t joined = 256 / (D / 4);   // rows a workgroup of the join
+  if (sets * p->slots > 0x7fffffff || rows * units > 0x7fffffff ||
+      sets * target * kThreads > kMaxThreads ||
+      (target > 1 && (rows + joined - 1) / joined * units * 256 > kMaxThreads))
+    return false;
   const size_t cells = (size_t)layers * heads * p->slots * p->rows_pad;
   p->off_ml = target > 1 ? cells * (size_t)D * sizeof(float) : 0;
   p->total = target > 1 ? p->off_ml + ((cells * sizeof(float2) + 15) & ~(size_t)15) : 0;

@@ -232,7 +232,7 @@ hipError_t launch_rows(const CacheRowsArgs& a, F64 f64, F128 f128, hipStream_t s
   const int64_t rows = (int64_t)a.layers * a.n * a.c.heads * a.max_count;
   if (rows == 0) return hipSuccess;
   const int64_t blocks = (rows * (a.c.D / 8) + kThreads - 1) / kThreads;
-  if (blocks > 0x7fffffff) return hipErrorInvalidValue;
+  if (blocks * kThreads > kMaxThreads) return hipErrorInvalidValue;
   if (a.c.D == 64) f64<<<(unsigned)blocks, kThreads, 0, s>>>(a);
   else f128<<<(unsigned)blocks, kThreads, 0, s>>>(a);
   return hipGetLastError();

@@ -217,6 +217,22 @@ def test_cache_calls_refuse_bad_arguments(cb):
     assert f["attend"](big, ws=FAKE + 8) == -6
 
 
+def test_calls_refuse_sizes_past_a_launch(cb):
+    """A grid holds 2^32 - 1 threads along an axis; a scale that fp32 holds, but not times log2(e)."""
+    f, c = calls(cb), L(desc(cb))
+    for name in ("write", "read"):                       # 8 units of 8 threads a row
+        assert f[name](c, most=(2**32 - 256) // 64 + 1) == -2
+    assert f["free"](c, n=2**24) == -2
+    for size in ((1, 1, 2**29), (2**10, 2**10, 2**30)):
+        assert cb._lib.cb_rotary(L(rows(cb, size=size)), 1, 64, FAKE, 64, 1.0, 0, 0, 1, None) == -2
+    assert f["attend"](c, seqs=FAKE, n=2**20, m=64) == -2      # 2^26 workgroups of the join
+    many = L(desc(cb, layers=4096, kv_heads=4096))
+    assert f["attend"](many, layers=4096, heads=4096, seqs=FAKE, n=2**20) == -2
+    need = cb._lib.cb_cache_attend_workspace_bytes
+    assert need(many, 4096, 2**20, 4096, 2**26) == need(c, 2, 2**20, 4, 64) == 0
+    assert f["attend"](c, scale=3e38) == -2
+
+
 def test_status_refuses(cb):
     assert cb._lib.cb_cache_status(None, None) == -1
     assert cb._lib.cb_cache_status(FAKE + 2, None) == -6
