@@ -95,12 +95,14 @@ class _rope(ctypes.Structure):
 
 
 class cb_rows(ctypes.Structure):
+    dev = None   # device of its tensors, where rows() made it
     _fields_ = [("x", _vp), ("out", _vp), ("pos", _vp), ("frm", _vp), ("size", _i64 * 3),
                 ("in_stride", _i64 * 3), ("out_stride", _i64 * 3), ("pos_stride", _i64 * 3),
                 ("from_stride", _i64 * 3)]
 
 
 class cb_cache(ctypes.Structure):
+    dev = None   # device of its tensors, where cache() made it
     _fields_ = [("layers", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
                 ("head_dim", ctypes.c_int32), ("page_len", ctypes.c_int32),
                 ("pages", ctypes.c_int32), ("seqs", ctypes.c_int32), ("width", ctypes.c_int32),
@@ -429,6 +431,14 @@ def _now(stream):
     return dev, stream if isinstance(stream, int) else stream.cuda_stream
 
 
+def _cache_now(c, where, stream):
+    """_now for a call on a cache, which has to be the current device's."""
+    dev, s = _now(stream)
+    if c.dev != dev and c.dev is not None:
+        raise CBError(-2, f"{where}: the cache is on device {c.dev}, the current one is {dev}")
+    return dev, s
+
+
 def _refuse(where, x, what, status=-2):
     raise CBError(status, f"{where}: {what} (got {tuple(x.shape)} {x.dtype} on {x.device})")
 
@@ -483,12 +493,13 @@ def cb_rotary_frequencies(rotary_dim: int, base: float = 10000.0, scaling: str =
     kinds = {"none": 0, "linear": 1, "yarn": 2}
     if scaling not in kinds:
         raise CBError(-2, f"cb_rotary_frequencies: scaling {scaling!r}")
-    r = _rope(int(rotary_dim), kinds[scaling], float(base), float(factor), float(original_len),
+    rotary_dim = max(-1, min(int(rotary_dim), 1 << 20))
+    r = _rope(rotary_dim, kinds[scaling], float(base), float(factor), float(original_len),
               float(fast_turns), float(slow_turns))
-    freq, amp = array.array("d", bytes(8 * max(0, min(int(rotary_dim), 1024) // 2 + 1))), ctypes.c_double(0.0)
+    freq, amp = array.array("d", bytes(8 * max(0, min(rotary_dim, 1024) // 2 + 1))), ctypes.c_double(0.0)
     _check(_lib.cb_rotary_frequencies(ctypes.byref(r), freq.buffer_info()[0], ctypes.byref(amp)),
            "cb_rotary_frequencies")
-    return list(freq[:int(rotary_dim) // 2]), amp.value
+    return list(freq[:rotary_dim // 2]), amp.value
 
 
 def rows(x, out, pos, frm=None) -> cb_rows:
@@ -498,15 +509,15 @@ def rows(x, out, pos, frm=None) -> cb_rows:
     where, torch = "rows", _torch or _lazy_torch()
     dev = torch.cuda.current_device()
     kind = _float_kind(x, where)
-    if x.dim() != 4 or out.shape != x.shape:
-        _refuse(where, out, f"rows [a][b][c][D] and their like are wanted, {tuple(x.shape)} given")
+    if x.dim() != 4 or out.shape != x.shape or x.shape[3] > 1024:
+        _refuse(where, out, f"rows [a][b][c][D <= 1024] and their like are wanted, {tuple(x.shape)} given")
     if out.dtype is not x.dtype:
         _refuse(where, out, f"{x.dtype} is wanted", -3)
     r = cb_rows(x=x.data_ptr(), out=out.data_ptr(), size=_S3(*x.shape[:3]),
                 in_stride=_S3(*_row_strides(x, where, dev)),
                 out_stride=_S3(*_row_strides(out, where, dev)))
     r.tensors = (x, out, pos, frm)
-    r.kind, r.head_dim = kind, x.shape[3]
+    r.kind, r.head_dim, r.dev = kind, x.shape[3], dev
     for p, name, stride in ((pos, "pos", "pos_stride"), (frm, "frm", "from_stride")):
         if p is not None:
             if p.dtype is not torch.int32:
@@ -539,10 +550,13 @@ def cb_rotary(parts, freq, amplitude: float = 1.0, interleaved: bool = False,
         if parts[1].head_dim != a.head_dim:
             raise CBError(-2, f"{where}: rows of unlike widths")
     dev, s = _now(stream)
+    for r in parts:
+        if r.dev != dev:
+            raise CBError(-2, f"{where}: rows on device {r.dev}, the current one is {dev}")
     if freq.dtype is not _torch.float64:
         _refuse(where, freq, "float64 frequencies are wanted", -3)
-    if freq.dim() != 1 or not freq.is_contiguous() or freq.get_device() != dev:
-        _refuse(where, freq, "a contiguous list on the current device is wanted")
+    if freq.dim() != 1 or freq.shape[0] > 512 or not freq.is_contiguous() or freq.get_device() != dev:
+        _refuse(where, freq, "a contiguous list of at most 512 on the current device is wanted")
     _check(_lib.cb_rotary((cb_rows * 2)(*parts) if n == 2 else _byref(a), n, a.head_dim,
                           freq.data_ptr(), 2 * freq.shape[0], amplitude, interleaved, transpose,
                           a.kind, s), where)
@@ -556,7 +570,8 @@ def cache(pool, refs, table, lens, head_dim: int, page_len: int) -> cb_cache:
     dev = torch.cuda.current_device()
     if pool.dtype is not torch.uint8 or table.dtype is not torch.int32:
         _refuse(where, pool, f"a uint8 pool and int32 tables are wanted, {table.dtype} given", -3)
-    if pool.dim() != 4 or pool.shape[3] != P * (D + D // 16) or table.dim() != 2:
+    if pool.dim() != 4 or pool.shape[3] != P * (D + D // 16) or table.dim() != 2 or \
+            max(*pool.shape, *table.shape) > 0x7fffffff:
         _refuse(where, pool, f"a pool [pages][layers][kv_heads][{P * (D + D // 16)}] is wanted")
     for t in (pool, table):
         if not t.is_contiguous() or t.get_device() != dev:
@@ -564,7 +579,7 @@ def cache(pool, refs, table, lens, head_dim: int, page_len: int) -> cb_cache:
     c = cb_cache(pool.shape[1], pool.shape[2], D, P, pool.shape[0], table.shape[0], table.shape[1],
                  0, pool.data_ptr(), _ints(refs, where, dev, pool.shape[0]), table.data_ptr(),
                  _ints(lens, where, dev, table.shape[0]))
-    c.tensors = (pool, refs, table, lens)
+    c.tensors, c.dev = (pool, refs, table, lens), dev
     if _lib.cb_cache_page_bytes(_byref(c)) == 0:
         raise CBError(-2, where)
     return c
@@ -600,7 +615,7 @@ def cb_cache_status(status, stream=None) -> int:
 
 def cb_cache_extend(c: cb_cache, seqs, add, status, stream=None) -> None:
     where = "cb_cache_extend"
-    dev, s = _now(stream)
+    dev, s = _cache_now(c, where, stream)
     n = seqs.numel()
     _check(_lib.cb_cache_extend(_byref(c), _ints(seqs, where, dev), _ints(add, where, dev, n), n,
                                 _ints(status, where, dev, 1), s), where)
@@ -608,7 +623,7 @@ def cb_cache_extend(c: cb_cache, seqs, add, status, stream=None) -> None:
 
 def cb_cache_free(c: cb_cache, seqs, stream=None) -> None:
     where = "cb_cache_free"
-    dev, s = _now(stream)
+    dev, s = _cache_now(c, where, stream)
     _check(_lib.cb_cache_free(_byref(c), _ints(seqs, where, dev), seqs.numel(), s), where)
 
 
@@ -619,7 +634,7 @@ def cb_cache_fork_workspace_bytes(c: cb_cache, n: int) -> int:
 def cb_cache_fork(c: cb_cache, parents, children, status, ws, copy: bool = False, ws_bytes=None,
                   stream=None) -> None:
     where = "cb_cache_fork"
-    dev, s = _now(stream)
+    dev, s = _cache_now(c, where, stream)
     n = parents.numel()
     _check(_lib.cb_cache_fork(_byref(c), _ints(parents, where, dev), _ints(children, where, dev, n),
                               n, copy, _ints(status, where, dev, 1),
@@ -634,7 +649,7 @@ def cb_cache_compact(c: cb_cache, src, dst, idx, status, ws, counts=None, ws_byt
                      stream=None) -> None:
     """idx: int32 [n][layers or 1][kv_heads or 1][keep]; an axis of one serves all."""
     where = "cb_cache_compact"
-    dev, s = _now(stream)
+    dev, s = _cache_now(c, where, stream)
     n = src.numel()
     if idx.dtype is not _torch.int32:
         _refuse(where, idx, "int32 positions are wanted", -3)
@@ -651,11 +666,12 @@ def cb_cache_compact(c: cb_cache, src, dst, idx, status, ws, counts=None, ws_byt
 
 
 def _cache_rows(fn, where, c, k, v, seqs, start, counts, layer, stream):
-    dev, s = _now(stream)
+    dev, s = _cache_now(c, where, stream)
     kind, shape = _float_kind(k, where), k.shape
-    if len(shape) != 5 or shape[2] != c.kv_heads or shape[4] != c.head_dim or v.shape != shape:
+    if len(shape) != 5 or shape[2] != c.kv_heads or shape[4] != c.head_dim or v.shape != shape or \
+            max(shape) > 0x7fffffff or not 0 <= layer < 4096:
         _refuse(where, v, f"rows [layers][n][{c.kv_heads}][rows][{c.head_dim}] are wanted, keys and "
-                          f"values alike, {tuple(shape)} given")
+                          f"values alike, {tuple(shape)} at layer {layer} given")
     if v.dtype is not k.dtype:
         _refuse(where, v, f"{k.dtype} is wanted", -3)
     st = _row_strides(k, where, dev)
@@ -690,11 +706,12 @@ def cb_cache_attend(c: cb_cache, q, out, ws=None, lse=None, seqs=None, q_lens=No
                     stream=None) -> None:
     """q, out [layers][n][q_heads][q_len][D]; lse [layers][n][q_heads][q_len] fp32."""
     where = "cb_cache_attend"
-    dev, s = _now(stream)
+    dev, s = _cache_now(c, where, stream)
     kind, shape = _float_kind(q, where), q.shape
-    if len(shape) != 5 or shape[4] != c.head_dim or out.shape != shape:
+    if len(shape) != 5 or shape[4] != c.head_dim or out.shape != shape or \
+            max(shape) > 0x7fffffff or not 0 <= layer < 4096:
         _refuse(where, out, f"rows [layers][n][q_heads][q_len][{c.head_dim}] and their like are wanted, "
-                            f"{tuple(shape)} given")
+                            f"{tuple(shape)} at layer {layer} given")
     if out.dtype is not q.dtype:
         _refuse(where, out, f"{q.dtype} is wanted", -3)
     qs, os_ = _row_strides(q, where, dev), _row_strides(out, where, dev)

@@ -711,6 +711,32 @@ def test_calls_refuse_tensors(torch, cb):
             bad()
 
 
+def test_calls_refuse_other_devices_and_wide_sizes(torch, cb):
+    """A cache or rows described on another device than the current one; sizes that C takes in 32 bits."""
+    c = cache_with(torch, cb, [20], D=64, P=16)
+    k = torch.zeros((1, 1, 2, 3, 64), device="cuda")
+    one, wide = ints(torch, [0]), k[:, :, :, :1].expand(1, 2**32 + 1, 2, 1, 64)
+    freq = torch.zeros(2**10, dtype=torch.float64, device="cuda")
+    moved = cb.rows(k[0], k[0], one)
+    moved.dev = 1   # as if made there
+    for bad in [lambda: cb.cb_rotary(moved, freq[:32]), lambda: cb.cb_rotary(cb.rows(k[0], k[0], one), freq),
+                lambda: cb.cb_cache_write(c.desc, wide, wide), lambda: cb.cb_cache_read(c.desc, k, k.clone(), layer=2**32),
+                lambda: cb.cb_cache_attend(c.desc, k, k.clone(), layer=2**32),
+                lambda: cb.cb_cache_attend(c.desc, wide, wide),
+                lambda: cb.cb_rotary_frequencies(2**32 + 64)]:
+        with pytest.raises(cb.CBError):
+            bad()
+    c.desc.dev = 1
+    ws = torch.zeros(1 << 12, dtype=torch.uint8, device="cuda")
+    idx = torch.zeros((1, 1, 1, 4), dtype=torch.int32, device="cuda")
+    for bad in [lambda: cb.cb_cache_write(c.desc, k, k), lambda: cb.cb_cache_read(c.desc, k, k.clone()),
+                lambda: cb.cb_cache_attend(c.desc, k, k.clone()), lambda: cb.cb_cache_extend(c.desc, one, one, c.status),
+                lambda: cb.cb_cache_free(c.desc, one), lambda: cb.cb_cache_fork(c.desc, one, one, c.status, ws),
+                lambda: cb.cb_cache_compact(c.desc, one, one, idx, c.status, ws)]:
+        with pytest.raises(cb.CBError, match="current one is 0"):
+            bad()
+
+
 # ---- all of it together -----------------------------------------------------------
 
 
