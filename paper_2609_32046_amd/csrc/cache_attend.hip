@@ -21,6 +21,14 @@
 // (each workgroup finds its own from the lengths).  Four waves take a run's steps in
 // turn; their results meet in LDS, and those of a sequence that several runs
 // share in a second, small kernel.
+//
+// Few rows are bound by HBM: 64 sequences of up to 16384 positions (606 MB) take 121 us in all,
+// 5.0 TB/s, against 109 us with the loads alone; one of 131072 (143 MB) takes 31 us and 5 us of
+// joining.  Many rows are bound by issue: a step of 64 rows is 64 MFMAs (1060 cycles), 32
+// exponentials (380) and about 250 other vector instructions (1150), and the two waves of a
+// SIMD overlap little of it: 2500 rows (500 tokens of 40 heads) over 32768 positions
+// take 356 us, 940 TFLOP/s.  Tried for them and slower: conversions shared through LDS
+// (416-459 us), 32 x 32 x 16 MFMAs (402 us), waves with rows of their own (371 us).
 #include <math.h>
 
 #include "cache.h"
@@ -781,7 +789,7 @@ bool make_attend_plan(int layers, int n, int heads, int q_heads, int64_t q_len, 
   if (rows > (1 << 26) || units > 0x7fffffff) return false;
   // no run shorter than kShortest rounds even where every sequence is full
   const int64_t most = (int64_t)n * ((capacity + kShortest * kRound - 1) / (kShortest * kRound));
-  // Blocks of a wave share a step's conversions; with fp32 rows two do not fit the
+  // Blocks of a wave share a step's conversions (64 instructions); with fp32 rows two do not fit the
   // registers at D = 128.  A call that cannot fill the device takes one block to a wave: more
   // workgroups, each sooner done (32 fp32 rows over 512 positions: 7.2 us, 10.3 with two).
   const int64_t single = (rows + 15) / 16 * heads * layers;

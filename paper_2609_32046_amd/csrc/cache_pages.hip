@@ -6,7 +6,9 @@
 // right, and every call's outcome is a function of it.  A call that takes pages
 // plans in one workgroup (it checks every entry before it changes anything,
 // and takes back what it released when pages lack), then moves bytes with the
-// whole device.
+// whole device.  A plan is a chain of reads that wait for one another (list, length, row, count):
+// 9 us to extend 64 sequences, 13 to fork 64 children of 32 pages, 8-10 to compact; giving
+// back 64 sequences takes 5.
 #include "cache.h"
 
 namespace cb {
@@ -496,7 +498,10 @@ __global__ __launch_bounds__(kPlan) void cache_compact_plan_kernel(CacheCompactA
 
 // 16 new positions of one unit a wave: 16 rows of key codes by four (D = 128) or
 // two (64) lanes of 16 bytes; four lanes' blocks of value codes, each lane's 16 (8)
-// bytes from the four positions' own places.
+// bytes from the four positions' own places.  Bound by HBM in lines of 128 bytes: a quarter of
+// three messages of 8192 positions (36 layers, 8 heads: 240 MB kept) takes 151 us, in which 574 MB are
+// read and 240 written, 5.4 TB/s: a kept row's 64 bytes of key codes share their line with a
+// neighbour's, its value codes lie in two lines of a block of four positions.
 template <int D>
 __global__ __launch_bounds__(256) void cache_gather_kernel(CacheCompactArgs a, int blocks_per_unit,
                                                            int64_t items) {
