@@ -101,6 +101,7 @@ struct AttendArgs {
   int32_t layer0, layers, n, q_heads, group;
   int32_t row_tiles, rows_pad;
   int32_t target;   // runs that the positions are dealt to
+  int32_t whole;    // a run is a sequence
   int32_t slots;    // target + n
   int32_t causal;
   float c2;         // scale * log2(e)
@@ -110,6 +111,7 @@ struct AttendArgs {
 struct AttendPlan {
   int32_t blocks;   // 16-row blocks a wave holds
   int32_t row_tiles, rows_pad, target, slots;
+  bool whole;       // no sequence is cut
   size_t off_ml, total;
 };
 

@@ -383,6 +383,7 @@ int cb_cache_attend(const cb_cache* c, int32_t layer0, int32_t layers, const int
   a.row_tiles = p.row_tiles;
   a.rows_pad = p.rows_pad;
   a.target = p.target;
+  a.whole = p.whole;
   a.slots = p.slots;
   a.causal = causal != 0;
   a.c2 = fmaxf((float)c2, 1e-37f);   // never 0: a masked logit is -inf times it

@@ -146,6 +146,10 @@ __device__ inline int64_t rounds_per_run(const AttendArgs& a, int64_t* total) {
 }
 
 __device__ inline bool find_run(const AttendArgs& a, int run, Run* r) {
+  if (a.whole) {   // a run a sequence
+    *r = {run, 0, 0, rounds_of(uniform_len(a, run))};
+    return true;
+  }
   int64_t total;
   const int64_t per = rounds_per_run(a, &total);
   r->lo = run * per;
@@ -778,9 +782,14 @@ constexpr int64_t kUnits = 256;
 // Rounds of the shortest run: 16 sequences of 1024 positions take 16.3 us in runs of two
 // rounds, 18.4 of four, 21.8 of eight.
 constexpr int64_t kShortest = 2;
-// One sequence of up to so many rounds stays whole, and nothing is joined: 1024 positions take
-// 11.3 us so and 14.6 cut, 2048 positions 15.0 with runs that long and 13.5 with short ones.
-constexpr int64_t kWhole = 8;
+// Where no sequence can be longer than so many rounds, each stays whole, a run of its own, and
+// nothing is joined: kWhole of them where the workgroups are few, up to kWholeFull where they
+// fill half the device.  Decoding over 8 KV heads, cut and whole: one of 1024 positions 14.6 and
+// 11.3 us, of 2048 13.5 and 16.1; 16 of 2048 17.7 and 15.8, of 4096 21.6 and 26.5; 64 of 1024
+// 25.1 and 14.7, of 4096 39.4 and 36.0.  128 tokens of 32 heads behind 300 positions, 64 times:
+// 190 and 138.  Longer ones are cut however many they are: one among many short ones would be
+// a single workgroup's work.
+constexpr int64_t kWhole = 8, kWholeFull = 32;
 
 bool make_attend_plan(int layers, int n, int heads, int q_heads, int64_t q_len, int D, bool f32,
                       int64_t capacity, AttendPlan* p) {
@@ -813,7 +822,11 @@ bool make_attend_plan(int layers, int n, int heads, int q_heads, int64_t q_len, 
     }
   }
   if (target > most) target = most;
-  if (n == 1 && capacity <= kWhole * kRound) target = 1;
+  const int64_t longest = (capacity + kRound - 1) / kRound, groups = sets * n;
+  p->whole = longest <= kWholeFull && groups * kThreads <= kMaxThreads &&
+             longest <= kWhole + (kWholeFull - kWhole) * groups / (resident / 2);
+  if (p->whole) target = n;
+  const bool joins = target > 1 && !p->whole;
   p->row_tiles = (int32_t)tiles;
   p->rows_pad = (int32_t)(tiles * per);
   p->target = (int32_t)target;
@@ -822,11 +835,11 @@ bool make_attend_plan(int layers, int n, int heads, int q_heads, int64_t q_len, 
   const int64_t joined = 256 / (D / 4);   // rows a workgroup of the join
   if (sets * p->slots > 0x7fffffff || rows * units > 0x7fffffff ||
       sets * target * kThreads > kMaxThreads ||
-      (target > 1 && (rows + joined - 1) / joined * units * 256 > kMaxThreads))
+      (joins && (rows + joined - 1) / joined * units * 256 > kMaxThreads))
     return false;
   const size_t cells = (size_t)layers * heads * p->slots * p->rows_pad;
-  p->off_ml = target > 1 ? cells * (size_t)D * sizeof(float) : 0;
-  p->total = target > 1 ? p->off_ml + ((cells * sizeof(float2) + 15) & ~(size_t)15) : 0;
+  p->off_ml = joins ? cells * (size_t)D * sizeof(float) : 0;
+  p->total = joins ? p->off_ml + ((cells * sizeof(float2) + 15) & ~(size_t)15) : 0;
   return true;
 }
 

@@ -210,7 +210,7 @@ def test_cache_calls_refuse_bad_arguments(cb):
                       (dict(lse=FAKE + 2), -6), (dict(qs=wrong4), -6), (dict(os_=wrong4), -6),
                       (dict(os_=zero4), -2), (dict(q_lens=FAKE + 2), -6)]:
         assert f["attend"](c, **bad) == code, bad
-    big = L(desc(cb, width=64))   # long enough to be cut into chunks
+    big = L(desc(cb, width=65))   # long enough to be cut into chunks
     need = cb._lib.cb_cache_attend_workspace_bytes(big, 2, 2, 4, 4)
     assert need > 0
     assert f["attend"](big, ws=None, ws_bytes=0) == -5 and f["attend"](big, dtype=0, ws_bytes=15) == -5
@@ -225,11 +225,12 @@ def test_calls_refuse_sizes_past_a_launch(cb):
     assert f["free"](c, n=2**24) == -2
     for size in ((1, 1, 2**29), (2**10, 2**10, 2**30)):
         assert cb._lib.cb_rotary(L(rows(cb, size=size)), 1, 64, FAKE, 64, 1.0, 0, 0, 1, None) == -2
-    assert f["attend"](c, seqs=FAKE, n=2**20, m=64) == -2      # 2^26 workgroups of the join
+    long = L(desc(cb, width=4096))
+    assert f["attend"](long, seqs=FAKE, n=2**20, m=64) == -2   # 2^26 workgroups of the join
     many = L(desc(cb, layers=4096, kv_heads=4096))
     assert f["attend"](many, layers=4096, heads=4096, seqs=FAKE, n=2**20) == -2
     need = cb._lib.cb_cache_attend_workspace_bytes
-    assert need(many, 4096, 2**20, 4096, 2**26) == need(c, 2, 2**20, 4, 64) == 0
+    assert need(many, 4096, 2**20, 4096, 2**26) == need(long, 2, 2**20, 4, 64) == 0
     assert f["attend"](c, scale=3e38) == -2
 
 
@@ -246,6 +247,8 @@ def test_sizes(cb):
         assert fn(L(desc(cb, width=0)), 3) == 0
     n = cb._lib.cb_cache_attend_workspace_bytes
     assert n(L(desc(cb)), 1, 1, 4, 1) == 0                       # 64 positions: no split
+    assert n(L(desc(cb, width=64)), 1, 3, 4, 1) == 0             # 1024 neither
+    assert n(L(desc(cb, width=65)), 1, 3, 4, 1) > 0
     assert n(L(desc(cb, width=4096)), 1, 1, 4, 1) > 0
     assert n(L(desc(cb, width=4096)), 1, 1, 3, 1) == 0           # refused by the call
 

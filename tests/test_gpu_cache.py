@@ -511,8 +511,10 @@ def scratch(torch, cb, c, q):
 
 
 def attend_case(torch, cb, lens, Hkv, G, D, P, m, dtype, causal, seqs=None, q_lens=None, layers=1, layer0=0,
-                scale=0.0, seed=0, holes=(), prepare=None, extra=3):
-    c = cache_with(torch, cb, lens, L=layers + layer0, H=Hkv, D=D, P=P, seed=seed, extra=extra)
+                scale=0.0, seed=0, holes=(), prepare=None, extra=3, cut=False):
+    """cut: a table of more than 4096 positions, whose sequences are cut into runs, however short they are."""
+    c = cache_with(torch, cb, lens, L=layers + layer0, H=Hkv, D=D, P=P, seed=seed, extra=extra,
+                   width=8192 // P if cut else None)
     fill_cache(torch, cb, c, lens, seed, layers + layer0)
     for s, j in holes:
         c.table[s, j] = -1
@@ -533,25 +535,27 @@ def attend_case(torch, cb, lens, Hkv, G, D, P, m, dtype, causal, seqs=None, q_le
     return c, q, out, lse, ws
 
 
+@pytest.mark.parametrize("cut", [False, True])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("D,P,Hkv,G", [(128, 64, 2, 4), (64, 16, 2, 2), (128, 16, 1, 5), (64, 128, 3, 1),
                                        (128, 256, 1, 8), (64, 32, 1, 17)])
-def test_attend_single_tokens(torch, cb, dtype, D, P, Hkv, G):
+def test_attend_single_tokens(torch, cb, dtype, D, P, Hkv, G, cut):
     """Decoding: one query token a sequence, every length around the tiles and pages."""
     lens = [0, 1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 256, 257, 300]
-    attend_case(torch, cb, lens, Hkv, G, D, P, 1, dtype, True, seed=D + P + G)
+    attend_case(torch, cb, lens, Hkv, G, D, P, 1, dtype, True, seed=D + P + G, cut=cut)
 
 
+@pytest.mark.parametrize("cut", [False, True])
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("D,P,G,m", [(128, 32, 4, 5), (64, 16, 3, 7), (128, 16, 1, 33), (64, 64, 8, 20), (128, 128, 5, 50),
                                        (64, 16, 7, 40), (128, 32, 8, 65)])
-def test_attend_several_tokens(torch, cb, causal, dtype, D, P, G, m):
+def test_attend_several_tokens(torch, cb, causal, dtype, D, P, G, m, cut):
     """Prompts' parts: more query tokens than positions (rows of no position), ragged query counts, one
     of none, sequences named out of order and twice, the second layer."""
     lens = [40, 3, 0, 150, m]
     attend_case(torch, cb, lens, 2, G, D, P, m, dtype, causal, seqs=[3, 0, 4, 1, 3, 2, 0],
-                q_lens=[m, max(1, m // 2), m + 9, m, 0, m, -1], layers=1, layer0=1, seed=m + G)
+                q_lens=[m, max(1, m // 2), m + 9, m, 0, m, -1], layers=1, layer0=1, seed=m + G, cut=cut)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -568,6 +572,7 @@ def test_attend_many_sequences(torch, cb):
     """More sequences than lanes, so that the search for a chunk takes several rounds."""
     rng = np.random.default_rng(0)
     lens = [int(x) for x in rng.integers(0, 90, 150)] + [1200]
+    attend_case(torch, cb, lens, 1, 2, 64, 16, 1, "bf16", True, seed=6, cut=True)
     attend_case(torch, cb, lens, 1, 2, 64, 16, 1, "bf16", True, seed=6)
 
 
