@@ -112,6 +112,7 @@ struct AttendPlan {
   int32_t blocks;   // 16-row blocks a wave holds
   int32_t row_tiles, rows_pad, target, slots;
   bool whole;       // no sequence is cut
+  bool alone;       // a workgroup is one wave
   size_t off_ml, total;
 };
 

@@ -20,7 +20,9 @@
 // equal runs, however ragged they are: a run may end one sequence and begin the next
 // (each workgroup finds its own from the lengths).  Four waves take a run's steps in
 // turn; their results meet in LDS, and those of a sequence that several runs
-// share in a second, small kernel.
+// share in a second, small kernel.  Where the table bounds the sequences to short ones, a run
+// is a sequence and the second kernel falls away; where there are many, a workgroup is one
+// wave and nothing meets at all.
 //
 // Few rows are bound by HBM: 64 sequences of up to 16384 positions (606 MB) take 121 us in all,
 // 5.0 TB/s, against 109 us with the loads alone; one of 131072 (143 MB) takes 31 us and 5 us of
@@ -280,6 +282,22 @@ struct RowType<false> { typedef __bf16 type; };
 template <>
 struct RowType<true> { typedef float type; };
 
+// N neighbouring values of an output row: 4 or 8.
+template <int N>
+__device__ inline void put_row(float* p, const float (&x)[N]) {
+#pragma unroll
+  for (int v = 0; v < N; v += 4)
+    *reinterpret_cast<f32x4*>(p + v) = f32x4{x[v], x[v + 1], x[v + 2], x[v + 3]};
+}
+template <int N>
+__device__ inline void put_row(__bf16* p, const float (&x)[N]) {
+  uint32_t w[N / 2];
+#pragma unroll
+  for (int v = 0; v < N; v += 2) w[v / 2] = pack_bf16(x[v], x[v + 1]);
+  if constexpr (N == 8) *reinterpret_cast<u32x4*>(p) = u32x4{w[0], w[1], w[2], w[3]};
+  else *reinterpret_cast<u32x2*>(p) = u32x2{w[0], w[1]};
+}
+
 // Values of one tile pair (values 2b and 2b + 1 of the lane's run) for the step's 32 positions:
 // conversions give (value 2b, value 2b+1) of a position; the product wants pairs of
 // positions.
@@ -305,8 +323,8 @@ __device__ inline void value_tiles(const uint32_t (&wv)[2][D / 32], const float 
   *odd = __builtin_bit_cast(bf16x8, hi);
 }
 
-template <int D, bool F32, int RT>
-__global__ __launch_bounds__(kThreads, RT == 1 && !F32 ? 3 : 2) void attend_kernel(AttendArgs a) {
+template <int D, bool F32, int RT, int W>
+__global__ __launch_bounds__(64 * W, RT == 1 && !F32 ? 3 : 2) void attend_kernel(AttendArgs a) {
   typedef typename RowType<F32>::type T;
   constexpr int KS = D / 32;              // first product: MFMAs of a block and half
   constexpr int VT = D / 16;              // second: tiles of 16 values
@@ -314,8 +332,9 @@ __global__ __launch_bounds__(kThreads, RT == 1 && !F32 ? 3 : 2) void attend_kern
   constexpr int NB = RT == 1 && !F32 ? 3 : 2;     // steps of codes in registers, all but one under way
   constexpr bool kSharedQ = !F32 && RT > 1;       // the four waves' query rows are the same
   constexpr int kPad = 4;
-  __shared__ float so[kWaves][16][D + kPad];
-  __shared__ float sm[kWaves][RT * 16], sl[kWaves][RT * 16];
+  constexpr int kTurn = kStep * W;                // positions of a workgroup's step
+  __shared__ float so[W > 1 ? W : 1][W > 1 ? 16 : 1][D + kPad];
+  __shared__ float sm[W][RT * 16], sl[W][RT * 16];
   __shared__ bf16x8 sq[kSharedQ ? RT : 1][KS][kSharedQ ? 64 : 1];
 
   const int lane = threadIdx.x & 63;
@@ -385,7 +404,7 @@ __global__ __launch_bounds__(kThreads, RT == 1 && !F32 ? 3 : 2) void attend_kern
     for (int t = 0; t < RT; ++t) {
       if constexpr (kSharedQ) {
         // held in LDS, in the lanes' order: 16 reads a step of 64 rows, against 64 registers
-        if ((t & (kWaves - 1)) == wave) {
+        if (t % W == wave) {
           q[0].load(qp[t], g, live[t]);
 #pragma unroll
           for (int j = 0; j < KS; ++j) sq[t][j][lane] = q[0].x[j][0];
@@ -396,7 +415,7 @@ __global__ __launch_bounds__(kThreads, RT == 1 && !F32 ? 3 : 2) void attend_kern
     }
     if (kSharedQ) __syncthreads();
 
-    const int steps = hi <= lo ? 0 : (hi - lo + kRound - 1) / kRound;
+    const int steps = hi <= lo ? 0 : (hi - lo + kTurn - 1) / kTurn;
     // The page table through the scalar cache: its waits are apart from those for the codes,
     // so that these stay under way.  A half without a page (behind the end, or a
     // table entry that is none) reads page 0, in bounds, and is masked.  Steps behind the
@@ -405,12 +424,12 @@ __global__ __launch_bounds__(kThreads, RT == 1 && !F32 ? 3 : 2) void attend_kern
     const int mine = lo + wave * kStep;
     int id0 = 0, id1 = 0;
     auto look_up = [&](int k) {
-      const int t0 = mine + (k < steps ? k : steps - 1) * kRound, t1 = t0 + 16;
+      const int t0 = mine + (k < steps ? k : steps - 1) * kTurn, t1 = t0 + 16;
       id0 = row_pages[(t0 < hi ? t0 : hi - 1) >> a.c.page_shift];
       id1 = row_pages[(t1 < hi ? t1 : hi - 1) >> a.c.page_shift];
     };
     auto fetch = [&](int k, Raw<D>& w) {
-      const int t0 = mine + (k < steps ? k : steps - 1) * kRound;
+      const int t0 = mine + (k < steps ? k : steps - 1) * kTurn;
       const bool ok0 = t0 < hi && (unsigned)id0 < (unsigned)a.c.pages;
       const bool ok1 = t0 + 16 < hi && (unsigned)id1 < (unsigned)a.c.pages;
       w.here = (ok0 ? 1u : 0u) | (ok1 ? 2u : 0u);
@@ -436,7 +455,7 @@ __global__ __launch_bounds__(kThreads, RT == 1 && !F32 ? 3 : 2) void attend_kern
     }
 
     auto step = [&](int k, const Raw<D>& cur) {
-      const int t0 = lo + k * kRound + wave * kStep;
+      const int t0 = mine + k * kTurn;
       if (t0 >= hi) return;
       const bool masked = t0 + kStep > full || cur.here != 3u;   // uniform
       uint32_t vs[2] = {cur.vs[0], cur.vs[1]};
@@ -572,6 +591,33 @@ __global__ __launch_bounds__(kThreads, RT == 1 && !F32 ? 3 : 2) void attend_kern
         if (k0 + i < steps) step(k0 + i, raw[i]);
       }
 
+    if constexpr (W == 1) {
+      // the wave has its rows to itself: a lane's D/16 neighbouring values at a time
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+        sum[t] += __shfl_xor(sum[t], 16);
+        sum[t] += __shfl_xor(sum[t], 32);
+        const int row = row0 + t * 16 + r;
+        if (row >= rows) continue;
+        const float inv = sum[t] == 0.f ? 0.f : 1.f / sum[t];
+        const int tok = row / G;
+        const int qh = head * G + row - tok * G;
+        T* out = static_cast<T*>(a.out) + layer * a.out_stride[0] + b * a.out_stride[1] +
+                 qh * a.out_stride[2] + tok * a.out_stride[3];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float x[VT];
+#pragma unroll
+          for (int v = 0; v < VT; ++v) x[v] = o[t][v][i] * inv;
+          put_row<VT>(out + (4 * g + i) * VT, x);
+        }
+        if (a.lse && g == 0)
+          a.lse[(((int64_t)layer * a.n + b) * a.q_heads + qh) * a.q_len + tok] =
+              sum[t] == 0.f ? -INFINITY : (top[t] + log2f(sum[t])) * 0.69314718055994531f;
+      }
+      if (kSharedQ) __syncthreads();   // the next sequence writes the same LDS
+      continue;
+    }
     // The four lane groups' sums, then the four waves' results.
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
@@ -622,20 +668,9 @@ __global__ __launch_bounds__(kThreads, RT == 1 && !F32 ? 3 : 2) void attend_kern
           const int qh = head * G + row - tok * G;
           T* out = static_cast<T*>(a.out) + layer * a.out_stride[0] + b * a.out_stride[1] +
                    qh * a.out_stride[2] + tok * a.out_stride[3] + d0;
-          if constexpr (F32) {
 #pragma unroll
-            for (int v = 0; v < VT; v += 4)
-              *reinterpret_cast<f32x4*>(out + v) =
-                  f32x4{acc[v] * inv, acc[v + 1] * inv, acc[v + 2] * inv, acc[v + 3] * inv};
-          } else {
-            uint32_t w[VT / 2];
-#pragma unroll
-            for (int v = 0; v < VT; v += 2) w[v / 2] = pack_bf16(acc[v] * inv, acc[v + 1] * inv);
-            if constexpr (D == 128)
-              *reinterpret_cast<u32x4*>(out) = u32x4{w[0], w[1], w[2], w[3]};
-            else
-              *reinterpret_cast<u32x2*>(out) = u32x2{w[0], w[1]};
-          }
+          for (int v = 0; v < VT; ++v) acc[v] *= inv;
+          put_row<VT>(out, acc);
           if (a.lse && (threadIdx.x & 15) == 0)
             a.lse[(((int64_t)layer * a.n + b) * a.q_heads + qh) * a.q_len + tok] =
                 L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994531f;
@@ -753,9 +788,15 @@ hipError_t launch(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
   constexpr int kMost = !F32 ? 4 : D == 64 ? 2 : 1;   // blocks of a wave, as in make_attend_plan
   const int64_t grid = (int64_t)a.c.heads * a.row_tiles * a.target * a.layers;
   if (grid * kThreads > kMaxThreads) return hipErrorInvalidValue;
-  if (p.blocks == 1) attend_kernel<D, F32, 1><<<(unsigned)grid, kThreads, 0, s>>>(a);
-  else if (F32 || p.blocks == 2) attend_kernel<D, F32, kMost < 2 ? kMost : 2><<<(unsigned)grid, kThreads, 0, s>>>(a);
-  else attend_kernel<D, F32, kMost><<<(unsigned)grid, kThreads, 0, s>>>(a);
+  if (p.alone) {
+    if (p.blocks == 1) attend_kernel<D, F32, 1, 1><<<(unsigned)grid, 64, 0, s>>>(a);
+    else if (F32 || p.blocks == 2) attend_kernel<D, F32, kMost < 2 ? kMost : 2, 1><<<(unsigned)grid, 64, 0, s>>>(a);
+    else attend_kernel<D, F32, kMost, 1><<<(unsigned)grid, 64, 0, s>>>(a);
+    return hipGetLastError();
+  }
+  if (p.blocks == 1) attend_kernel<D, F32, 1, kWaves><<<(unsigned)grid, kThreads, 0, s>>>(a);
+  else if (F32 || p.blocks == 2) attend_kernel<D, F32, kMost < 2 ? kMost : 2, kWaves><<<(unsigned)grid, kThreads, 0, s>>>(a);
+  else attend_kernel<D, F32, kMost, kWaves><<<(unsigned)grid, kThreads, 0, s>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.total == 0) return e;   // one run: nothing to join
   // Pieces of a row: about the runs over the sequences.  A workgroup a row where few rows have
@@ -790,6 +831,12 @@ constexpr int64_t kShortest = 2;
 // 190 and 138.  Longer ones are cut however many they are: one among many short ones would be
 // a single workgroup's work.
 constexpr int64_t kWhole = 8, kWholeFull = 32;
+// And where the waves that the device holds are taken often enough for their length, once for every
+// kAlone rounds, a workgroup is one wave, which has its rows to itself: nothing meets in
+// LDS.  With four waves and with one: 64 times 128 tokens of 32 heads over 300 positions 139 and 70 us,
+// over 1000 188 and 135 (1.3 times for 8 rounds), 20 times over 1000 73 and 67, over
+// 4000 165 and 210; 150 decoding over 256 positions 14.8 and 13.9, over 768 22.4 and 28.1.
+constexpr int64_t kAlone = 8;
 
 bool make_attend_plan(int layers, int n, int heads, int q_heads, int64_t q_len, int D, bool f32,
                       int64_t capacity, AttendPlan* p) {
@@ -826,6 +873,7 @@ bool make_attend_plan(int layers, int n, int heads, int q_heads, int64_t q_len, 
   p->whole = longest <= kWholeFull && groups * kThreads <= kMaxThreads &&
              longest <= kWhole + (kWholeFull - kWhole) * groups / (resident / 2);
   if (p->whole) target = n;
+  p->alone = p->whole && longest * kWaves * resident <= kAlone * groups;
   const bool joins = target > 1 && !p->whole;
   p->row_tiles = (int32_t)tiles;
   p->rows_pad = (int32_t)(tiles * per);

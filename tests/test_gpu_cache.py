@@ -584,8 +584,24 @@ def test_attend_scale_and_large_logits(torch, cb):
     attend_case(torch, cb, [100, 400], 1, 2, 128, 16, 3, "bf16", True, scale=1e-30, seed=10)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D,P,G,m", [(128, 32, 4, 1), (64, 16, 2, 8), (128, 16, 3, 9), (64, 64, 8, 4), (128, 64, 4, 16),
+                                       (64, 32, 5, 25), (128, 128, 8, 17)])
+def test_attend_hundreds_of_short_sequences(torch, cb, dtype, D, P, G, m):
+    """So many that each wave takes rows of its own: 400 entries over eight sequences, most of no or one query
+    token, some of all."""
+    rng = np.random.default_rng(m)
+    lens = [0, 1, 16, 17, 33, 100, 128, 64]
+    q_lens = [int(x) for x in rng.choice([0, 0, 0, 1], 400)]
+    for i in range(8):
+        q_lens[50 * i + i] = [m, m + 3, (m + 1) // 2][i % 3]
+    attend_case(torch, cb, lens, 1, G, D, P, m, dtype, True, seqs=[i % 8 for i in range(400)], q_lens=q_lens,
+                seed=m + G + D)
+
+
+@pytest.mark.parametrize("many", [False, True])
 @pytest.mark.parametrize("dtype,G", [("bf16", 3), ("f32", 3), ("bf16", 20), ("bf16", 30)])
-def test_attend_masked_places_hold_anything(torch, cb, dtype, G):
+def test_attend_masked_places_hold_anything(torch, cb, dtype, G, many):
     """Positions behind the limit with NaN groups, infinite values and any bytes: rows that do not see
     them stay as they are, rows that do are NaN in the group's values (or wholly, for a key)."""
     D, P, lens, m = 128, 32, [75, 40], 12
@@ -605,7 +621,9 @@ def test_attend_masked_places_hold_anything(torch, cb, dtype, G):
         q = 38 - 32
         c.pool[int(pages[1, 1]), 0, :, 2 * n + q * 4 + 2] = 255
 
-    _, _, out, _, _ = attend_case(torch, cb, lens, 1, G, D, P, m, dtype, True, seed=11, prepare=spoil)
+    rest = 398 if many else 0                     # entries of no query token, beside which a workgroup is one wave
+    _, _, out, _, _ = attend_case(torch, cb, lens, 1, G, D, P, m, dtype, True, seed=11, prepare=spoil,
+                                  seqs=[0, 1] + [0] * rest, q_lens=[m, m] + [0] * rest)
     nan = torch.isnan(out[0, 0])                  # [heads][rows][D]
     assert nan[:, 7:, 32:64].all() and not nan[:, :7].any() and not nan[:, 7:, :32].any()
     nan = torch.isnan(out[0, 1])
