@@ -204,14 +204,17 @@ int cb_cache_read(const cb_cache* c, int32_t layer0, int32_t layers, const int32
  * 0 selects 1/sqrt(D).  dtype of q and out: CB_F32 or CB_BF16; logits, statistics
  * and sums in fp32; with CB_BF16 the weights enter the product with V in bf16,
  * with CB_F32 in 24 bits.  A position without a page counts for nothing.
- * ws: cb_cache_attend_workspace_bytes bytes, 16-byte aligned; its contents
- * need not be initialised.  Deterministic.  At most two kernels. */
+ * longest: what the caller knows of the lengths: sequences longer than this are
+ * taken to be this long (0: as long as the table allows).  Short sequences in a
+ * wide table are faster with it: none is cut, and no results are joined.
+ * ws: cb_cache_attend_workspace_bytes bytes (same `longest`), 16-byte aligned;
+ * its contents need not be initialised.  Deterministic.  At most two kernels. */
 size_t cb_cache_attend_workspace_bytes(const cb_cache* c, int32_t layers, int32_t n,
-                                       int32_t q_heads, int64_t q_len);
+                                       int32_t q_heads, int64_t q_len, int64_t longest);
 int cb_cache_attend(const cb_cache* c, int32_t layer0, int32_t layers, const int32_t* seqs,
                     int32_t n, const void* q, const int64_t q_stride[4], int32_t q_heads,
-                    const int32_t* q_lens, int64_t q_len, int32_t causal, double scale, void* out,
-                    const int64_t out_stride[4], float* lse, int32_t dtype, void* ws,
+                    const int32_t* q_lens, int64_t q_len, int32_t causal, int64_t longest,
+                    double scale, void* out, const int64_t out_stride[4], float* lse, int32_t dtype, void* ws,
                     size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus

@@ -128,9 +128,9 @@ for _name, _args, _res in [
                             ctypes.POINTER(_i64), _i32, _vp], ctypes.c_int),
         ("cb_cache_read", [_pc, _i32, _i32, _vp, _i32, _vp, _vp, _i64, _vp, _vp,
                            ctypes.POINTER(_i64), _i32, _vp], ctypes.c_int),
-        ("cb_cache_attend_workspace_bytes", [_pc, _i32, _i32, _i32, _i64], _sz),
+        ("cb_cache_attend_workspace_bytes", [_pc, _i32, _i32, _i32, _i64, _i64], _sz),
         ("cb_cache_attend", [_pc, _i32, _i32, _vp, _i32, _vp, ctypes.POINTER(_i64), _i32, _vp, _i64,
-                             _i32, ctypes.c_double, _vp, ctypes.POINTER(_i64), _vp, _i32, _vp, _sz,
+                             _i32, _i64, ctypes.c_double, _vp, ctypes.POINTER(_i64), _vp, _i32, _vp, _sz,
                              _vp], ctypes.c_int)]:
     getattr(_lib, _name).argtypes = _args
     getattr(_lib, _name).restype = _res
@@ -696,15 +696,16 @@ def cb_cache_read(c: cb_cache, k, v, seqs=None, start=None, counts=None, layer: 
 
 
 def cb_cache_attend_workspace_bytes(c: cb_cache, layers: int, n: int, q_heads: int,
-                                    q_len: int) -> int:
+                                    q_len: int, longest: int = 0) -> int:
     """Scratch bytes of cb_cache_attend (0: it needs none)."""
-    return _lib.cb_cache_attend_workspace_bytes(_byref(c), layers, n, q_heads, q_len)
+    return _lib.cb_cache_attend_workspace_bytes(_byref(c), layers, n, q_heads, q_len, longest)
 
 
 def cb_cache_attend(c: cb_cache, q, out, ws=None, lse=None, seqs=None, q_lens=None,
                     causal: bool = True, scale: float = 0.0, layer: int = 0, ws_bytes=None,
-                    stream=None) -> None:
-    """q, out [layers][n][q_heads][q_len][D]; lse [layers][n][q_heads][q_len] fp32."""
+                    stream=None, longest: int = 0) -> None:
+    """q, out [layers][n][q_heads][q_len][D]; lse [layers][n][q_heads][q_len] fp32.  longest: the
+    longest of the sequences, where the host knows it (scratch asked for with the same)."""
     where = "cb_cache_attend"
     dev, s = _cache_now(c, where, stream)
     kind, shape = _float_kind(q, where), q.shape
@@ -721,7 +722,7 @@ def cb_cache_attend(c: cb_cache, q, out, ws=None, lse=None, seqs=None, q_lens=No
     n = shape[1]
     _check(_lib.cb_cache_attend(_byref(c), layer, shape[0], _ints(seqs, where, dev, n), n,
                                 q.data_ptr(), _S4(*qs), shape[2], _ints(q_lens, where, dev, n),
-                                shape[3], causal, scale, out.data_ptr(), _S4(*os_),
+                                shape[3], causal, longest, scale, out.data_ptr(), _S4(*os_),
                                 None if lse is None else lse.data_ptr(), kind,
                                 *_scratch(ws, ws_bytes, where, dev), s), where)
 

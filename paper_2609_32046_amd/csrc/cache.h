@@ -103,6 +103,7 @@ struct AttendArgs {
   int32_t target;   // runs that the positions are dealt to
   int32_t whole;    // a run is a sequence
   int32_t slots;    // target + n
+  int32_t room;     // no sequence is longer
   int32_t causal;
   float c2;         // scale * log2(e)
 };
@@ -111,6 +112,7 @@ struct AttendArgs {
 struct AttendPlan {
   int32_t blocks;   // 16-row blocks a wave holds
   int32_t row_tiles, rows_pad, target, slots;
+  int32_t room;     // positions of the longest
   bool whole;       // no sequence is cut
   bool alone;       // a workgroup is one wave
   size_t off_ml, total;

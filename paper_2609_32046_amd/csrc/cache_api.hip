@@ -307,36 +307,37 @@ int cb_cache_read(const cb_cache* c, int32_t layer0, int32_t layers, const int32
 
 // Checks shared by the size query and the call.
 static int attend_plan(const cb_cache* c, int32_t layers, int32_t n, int32_t q_heads, int64_t q_len,
-                       int32_t dtype, cb::AttendPlan* p) {
+                       int64_t longest, int32_t dtype, cb::AttendPlan* p) {
   if (!c) return CB_ERR_NULL;
   if (!sizes_ok(c) || layers < 0 || layers > c->layers || n < 0 || n > (1 << 20) || q_heads < 1 ||
-      q_heads % c->kv_heads != 0 || q_len < 0 || q_len > (1 << 26))
+      q_heads % c->kv_heads != 0 || q_len < 0 || q_len > (1 << 26) || longest < 0)
     return CB_ERR_SHAPE;
   if (dtype != CB_F32 && dtype != CB_BF16) return CB_ERR_DTYPE;
   if (layers == 0 || n == 0 || q_len == 0) {
     *p = cb::AttendPlan{};
     return CB_OK;
   }
+  const int64_t room = (int64_t)c->width * c->page_len;
   return cb::make_attend_plan(layers, n, c->kv_heads, q_heads, q_len, c->head_dim, dtype == CB_F32,
-                              (int64_t)c->width * c->page_len, p)
+                              longest > 0 && longest < room ? longest : room, p)
              ? CB_OK
              : CB_ERR_SHAPE;
 }
 
 size_t cb_cache_attend_workspace_bytes(const cb_cache* c, int32_t layers, int32_t n,
-                                       int32_t q_heads, int64_t q_len) {
+                                       int32_t q_heads, int64_t q_len, int64_t longest) {
   cb::AttendPlan p;
   size_t most = 0;   // of either dtype
   for (int dtype : {CB_F32, CB_BF16})
-    if (attend_plan(c, layers, n, q_heads, q_len, dtype, &p) == CB_OK && p.total > most)
+    if (attend_plan(c, layers, n, q_heads, q_len, longest, dtype, &p) == CB_OK && p.total > most)
       most = p.total;
   return most;
 }
 
 int cb_cache_attend(const cb_cache* c, int32_t layer0, int32_t layers, const int32_t* seqs,
                     int32_t n, const void* q, const int64_t q_stride[4], int32_t q_heads,
-                    const int32_t* q_lens, int64_t q_len, int32_t causal, double scale, void* out,
-                    const int64_t out_stride[4], float* lse, int32_t dtype, void* ws,
+                    const int32_t* q_lens, int64_t q_len, int32_t causal, int64_t longest,
+                    double scale, void* out, const int64_t out_stride[4], float* lse, int32_t dtype, void* ws,
                     size_t ws_bytes, void* stream) {
   cb::AttendArgs a{};
   int st = view_of(c, &a.c);
@@ -344,7 +345,7 @@ int cb_cache_attend(const cb_cache* c, int32_t layer0, int32_t layers, const int
   st = layers_ok(c, layer0, layers, n);
   if (st != CB_OK) return st;
   cb::AttendPlan p;
-  st = attend_plan(c, layers, n, q_heads, q_len, dtype, &p);
+  st = attend_plan(c, layers, n, q_heads, q_len, longest, dtype, &p);
   if (st != CB_OK) return st;
   if (!seqs && n > c->seqs) return CB_ERR_SHAPE;
   const double c2 = (scale == 0.0 ? 1.0 / sqrt((double)c->head_dim) : scale) * 1.4426950408889634;
@@ -385,6 +386,7 @@ int cb_cache_attend(const cb_cache* c, int32_t layer0, int32_t layers, const int
   a.target = p.target;
   a.whole = p.whole;
   a.slots = p.slots;
+  a.room = p.room;
   a.causal = causal != 0;
   a.c2 = fmaxf((float)c2, 1e-37f);   // never 0: a masked logit is -inf times it
   return done(cb::launch_cache_attend(a, p, dtype == CB_F32, static_cast<hipStream_t>(stream)));

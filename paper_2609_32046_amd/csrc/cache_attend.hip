@@ -91,8 +91,7 @@ __device__ inline int seq_len(const AttendArgs& a, int b) {
   const int s = a.seqs ? a.seqs[b] : b;
   if ((unsigned)s >= (unsigned)a.c.seqs) return 0;
   const int len = a.c.lens[s];
-  const int64_t room = (int64_t)a.c.width << a.c.page_shift;
-  return len < 0 ? 0 : (int64_t)len < room ? len : (int)room;
+  return len < 0 ? 0 : len < a.room ? len : a.room;
 }
 
 // The same through the scalar cache, for a row that the whole wave asks for.
@@ -103,8 +102,7 @@ __device__ inline int uniform_len(const AttendArgs& a, int b) {
   const int s = seq_of(a, b);
   if ((unsigned)s >= (unsigned)a.c.seqs) return 0;
   const int len = ((ConstInts)a.c.lens)[s];
-  const int64_t room = (int64_t)a.c.width << a.c.page_shift;
-  return len < 0 ? 0 : (int64_t)len < room ? len : (int)room;
+  return len < 0 ? 0 : len < a.room ? len : a.room;
 }
 __device__ inline int query_tokens(const AttendArgs& a, int b) {
   const int m = a.q_lens ? ((ConstInts)a.q_lens)[b] : (int)a.q_len;
@@ -875,6 +873,7 @@ bool make_attend_plan(int layers, int n, int heads, int q_heads, int64_t q_len, 
   if (p->whole) target = n;
   p->alone = p->whole && longest * kWaves * resident <= kAlone * groups;
   const bool joins = target > 1 && !p->whole;
+  p->room = (int32_t)capacity;   // below 2^31 - 2^16
   p->row_tiles = (int32_t)tiles;
   p->rows_pad = (int32_t)(tiles * per);
   p->target = (int32_t)target;

@@ -158,8 +158,8 @@ def calls(cb):
         return f
 
     def attend(c, layer=0, layers=2, seqs=None, n=2, q=FAKE, qs=s4, heads=4, q_lens=None, m=4,
-               scale=0.0, out=FAKE, os_=s4, lse=None, dtype=1, ws=FAKE, ws_bytes=1 << 40):
-        return lib.cb_cache_attend(c, layer, layers, seqs, n, q, qs, heads, q_lens, m, 1, scale, out,
+               longest=0, scale=0.0, out=FAKE, os_=s4, lse=None, dtype=1, ws=FAKE, ws_bytes=1 << 40):
+        return lib.cb_cache_attend(c, layer, layers, seqs, n, q, qs, heads, q_lens, m, 1, longest, scale, out,
                                    os_, lse, dtype, ws, ws_bytes, None)
 
     return {"extend": extend, "free": free, "fork": fork, "compact": compact,
@@ -203,7 +203,7 @@ def test_cache_calls_refuse_bad_arguments(cb):
             assert f[name](c, **bad) == code, (name, bad)
     assert f["read"](c, stride=zero4) == -2
     for bad, code in [(dict(layer=-1), -2), (dict(layers=3), -2), (dict(n=-1), -2), (dict(n=4), -2),
-                      (dict(heads=3), -2), (dict(heads=0), -2), (dict(m=-1), -2), (dict(m=2**27), -2),
+                      (dict(heads=3), -2), (dict(heads=0), -2), (dict(m=-1), -2), (dict(m=2**27), -2), (dict(longest=-1), -2),
                       (dict(scale=-1.0), -2), (dict(scale=math.nan), -2), (dict(scale=math.inf), -2),
                       (dict(q=None), -1), (dict(out=None), -1), (dict(qs=None), -1), (dict(os_=None), -1),
                       (dict(dtype=7), -3), (dict(q=FAKE + 8), -6), (dict(out=FAKE + 8), -6),
@@ -211,7 +211,7 @@ def test_cache_calls_refuse_bad_arguments(cb):
                       (dict(os_=zero4), -2), (dict(q_lens=FAKE + 2), -6)]:
         assert f["attend"](c, **bad) == code, bad
     big = L(desc(cb, width=65))   # long enough to be cut into chunks
-    need = cb._lib.cb_cache_attend_workspace_bytes(big, 2, 2, 4, 4)
+    need = cb._lib.cb_cache_attend_workspace_bytes(big, 2, 2, 4, 4, 0)
     assert need > 0
     assert f["attend"](big, ws=None, ws_bytes=0) == -5 and f["attend"](big, dtype=0, ws_bytes=15) == -5
     assert f["attend"](big, ws=FAKE + 8) == -6
@@ -230,7 +230,7 @@ def test_calls_refuse_sizes_past_a_launch(cb):
     many = L(desc(cb, layers=4096, kv_heads=4096))
     assert f["attend"](many, layers=4096, heads=4096, seqs=FAKE, n=2**20) == -2
     need = cb._lib.cb_cache_attend_workspace_bytes
-    assert need(many, 4096, 2**20, 4096, 2**26) == need(long, 2, 2**20, 4, 64) == 0
+    assert need(many, 4096, 2**20, 4096, 2**26, 0) == need(long, 2, 2**20, 4, 64, 0) == 0
     assert f["attend"](c, scale=3e38) == -2
 
 
@@ -246,11 +246,13 @@ def test_sizes(cb):
         assert fn(L(desc(cb)), 3) > 0 and fn(L(desc(cb)), -1) == 0 and fn(L(desc(cb)), 2049) == 0
         assert fn(L(desc(cb, width=0)), 3) == 0
     n = cb._lib.cb_cache_attend_workspace_bytes
-    assert n(L(desc(cb)), 1, 1, 4, 1) == 0                       # 64 positions: no split
-    assert n(L(desc(cb, width=64)), 1, 3, 4, 1) == 0             # 1024 neither
-    assert n(L(desc(cb, width=65)), 1, 3, 4, 1) > 0
-    assert n(L(desc(cb, width=4096)), 1, 1, 4, 1) > 0
-    assert n(L(desc(cb, width=4096)), 1, 1, 3, 1) == 0           # refused by the call
+    assert n(L(desc(cb)), 1, 1, 4, 1, 0) == 0                     # 64 positions: no split
+    assert n(L(desc(cb, width=64)), 1, 3, 4, 1, 0) == 0           # 1024 neither
+    assert n(L(desc(cb, width=65)), 1, 3, 4, 1, 0) > 0
+    assert n(L(desc(cb, width=4096)), 1, 1, 4, 1, 0) > 0
+    assert n(L(desc(cb, width=4096)), 1, 1, 4, 1, 1024) == 0     # told that none is longer
+    assert n(L(desc(cb, width=4096)), 1, 1, 4, 1, -1) == 0       # refused by the call
+    assert n(L(desc(cb, width=4096)), 1, 1, 3, 1, 0) == 0         # refused by the call
 
 
 # ---- the reference itself -----------------------------------------------------

@@ -576,6 +576,24 @@ def test_attend_many_sequences(torch, cb):
     attend_case(torch, cb, lens, 1, 2, 64, 16, 1, "bf16", True, seed=6)
 
 
+def test_attend_told_the_longest(torch, cb):
+    """A bound on the lengths spares the scratch of a wide table and changes nothing of a bound that holds; a longer
+    sequence is taken to be as long as it says."""
+    lens, D, P, m = [0, 17, 1000, 130], 128, 16, 3
+    c, q, out, _, _ = attend_case(torch, cb, lens, 2, 3, D, P, m, "bf16", True, seed=33, cut=True)
+    for longest in (1000, 1001, 130, 1):
+        assert cb.cb_cache_attend_workspace_bytes(c.desc, 1, 4, 6, m, longest) == 0
+        out.fill_(7.0)
+        cb.cb_cache_attend(c.desc, q, out, longest=longest)
+        got = model(c, D, P)
+        got.lens = np.minimum(got.lens, longest)
+        check_attend(torch, got, q, out, None, [0, 1, 2, 3], [m] * 4, True, 0.0, 0, "bf16")
+    with pytest.raises(cb.CBError):
+        cb.cb_cache_attend(c.desc, q, out, longest=5000)   # cut after all: it needs scratch
+    with pytest.raises(cb.CBError):
+        cb.cb_cache_attend(c.desc, q, out, longest=-1)
+
+
 def test_attend_scale_and_large_logits(torch, cb):
     """A scale of its own; logits of several hundred; equal logits."""
     attend_case(torch, cb, [100, 400], 1, 2, 64, 16, 3, "f32", True, scale=0.31, seed=7)
