@@ -99,6 +99,7 @@ struct AttendArgs {
   int64_t q_stride[4], out_stride[4];
   int64_t q_len;    // m
   int32_t layer0, layers, n, q_heads, group;
+  uint32_t recip;   // floor(2^32 / group), or the most there is
   int32_t row_tiles, rows_pad;
   int32_t target;   // runs that the positions are dealt to
   int32_t whole;    // a run is a sequence

@@ -381,6 +381,7 @@ int cb_cache_attend(const cb_cache* c, int32_t layer0, int32_t layers, const int
   a.n = n;
   a.q_heads = q_heads;
   a.group = q_heads / c->kv_heads;
+  a.recip = a.group == 1 ? 0xffffffffu : (uint32_t)(((uint64_t)1 << 32) / (uint32_t)a.group);
   a.row_tiles = p.row_tiles;
   a.rows_pad = p.rows_pad;
   a.target = p.target;

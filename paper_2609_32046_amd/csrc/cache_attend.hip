@@ -109,6 +109,13 @@ __device__ inline int query_tokens(const AttendArgs& a, int b) {
   return m < 0 ? 0 : m < (int)a.q_len ? m : (int)a.q_len;
 }
 
+// Token of a query row, row / group: by the group's reciprocal, floor(2^32 / group), which gives
+// the quotient or one less; the compiler's own division takes four times the instructions.
+__device__ inline int token_of(const AttendArgs& a, int row) {
+  const int t = (int)__umulhi((uint32_t)row, a.recip);
+  return row - t * a.group >= a.group ? t + 1 : t;
+}
+
 // Rounds of a sequence; an empty one takes its turn too, to write its zeros.
 __device__ inline int rounds_of(int len) { return len <= kRound ? 1 : (len + kRound - 1) / kRound; }
 
@@ -375,14 +382,16 @@ __global__ __launch_bounds__(64 * W, RT == 1 && !F32 ? 3 : 2) void attend_kernel
     const int end = (int64_t)rhi * kRound < len ? rhi * kRound : len;
 
     // Limits of this lane's rows; the positions that all rows of the tile see, and that any sees.
+    int pr = r;
+    if constexpr (RT > 1) asm volatile("" : "+v"(pr));
     int limit[RT];
     const T* qp[RT];
     bool live[RT];
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-      const int row = row0 + t * 16 + r;
+      const int row = row0 + t * 16 + pr;
       live[t] = row < rows;
-      const int tok = live[t] ? row / G : 0;
+      const int tok = live[t] ? token_of(a, row) : 0;
       const int qh = head * G + (live[t] ? row - tok * G : 0);
       const int see = a.causal ? len - m + tok + 1 : len;
       limit[t] = !live[t] || see < 0 ? 0 : see < end ? see : end;
@@ -391,8 +400,8 @@ __global__ __launch_bounds__(64 * W, RT == 1 && !F32 ? 3 : 2) void attend_kernel
     }
     // rows ascend with tokens, so the first row sees least, the last live one most
     const int row_last = (row0 + RT * 16 < rows ? row0 + RT * 16 : rows) - 1;
-    const int see_first = a.causal ? len - m + row0 / G + 1 : len;
-    const int see_last = a.causal ? len - m + row_last / G + 1 : len;
+    const int see_first = a.causal ? len - m + token_of(a, row0) + 1 : len;
+    const int see_last = a.causal ? len - m + token_of(a, row_last) + 1 : len;
     const int full = see_first < end ? (see_first > 0 ? see_first : 0) : end;
     const int hi = see_last < end ? (see_last > 0 ? see_last : 0) : end;
 
@@ -591,14 +600,16 @@ __global__ __launch_bounds__(64 * W, RT == 1 && !F32 ? 3 : 2) void attend_kernel
 
     if constexpr (W == 1) {
       // the wave has its rows to itself: a lane's D/16 neighbouring values at a time
+      int er = r;
+      if constexpr (RT > 1) asm volatile("" : "+v"(er));
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
         sum[t] += __shfl_xor(sum[t], 16);
         sum[t] += __shfl_xor(sum[t], 32);
-        const int row = row0 + t * 16 + r;
+        const int row = row0 + t * 16 + er;
         if (row >= rows) continue;
         const float inv = sum[t] == 0.f ? 0.f : 1.f / sum[t];
-        const int tok = row / G;
+        const int tok = token_of(a, row);
         const int qh = head * G + row - tok * G;
         T* out = static_cast<T*>(a.out) + layer * a.out_stride[0] + b * a.out_stride[1] +
                  qh * a.out_stride[2] + tok * a.out_stride[3];
@@ -616,14 +627,19 @@ __global__ __launch_bounds__(64 * W, RT == 1 && !F32 ? 3 : 2) void attend_kernel
       if (kSharedQ) __syncthreads();   // the next sequence writes the same LDS
       continue;
     }
-    // The four lane groups' sums, then the four waves' results.
+    // The four lane groups' sums, then the four waves' results.  With several blocks the thread's
+    // number is taken anew, or what follows from it would be worked out before the loop and
+    // spilled.
+    int tid = (int)threadIdx.x;
+    if constexpr (RT > 1) asm volatile("" : "+v"(tid));
+    const int er = tid & 15, eg = (tid >> 4) & 3;
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
       sum[t] += __shfl_xor(sum[t], 16);
       sum[t] += __shfl_xor(sum[t], 32);
-      if (g == 0) {
-        sm[wave][t * 16 + r] = top[t];
-        sl[wave][t * 16 + r] = sum[t];
+      if (eg == 0) {
+        sm[wave][t * 16 + er] = top[t];
+        sl[wave][t * 16 + er] = sum[t];
       }
     }
     // run and sequence both ascend, so their sum names a piece
@@ -637,11 +653,11 @@ __global__ __launch_bounds__(64 * W, RT == 1 && !F32 ? 3 : 2) void attend_kernel
         for (int v = 0; v < VT; v += 4) {
           // values (4g + i) * D/16 + v ..: one from each of four tiles
           const f32x4 x = {o[t][v][i], o[t][v + 1][i], o[t][v + 2][i], o[t][v + 3][i]};
-          *reinterpret_cast<f32x4*>(&so[wave][r][(4 * g + i) * VT + v]) = x;
+          *reinterpret_cast<f32x4*>(&so[wave][er][(4 * eg + i) * VT + v]) = x;
         }
       __syncthreads();
       // thread: row tid / 16, D/16 of its values
-      const int qr = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * VT;
+      const int qr = tid >> 4, d0 = (tid & 15) * VT;
       const int row = row0 + t * 16 + qr;
       float mw[kWaves], M = kNone, L = 0.f;
 #pragma unroll
@@ -662,14 +678,14 @@ __global__ __launch_bounds__(64 * W, RT == 1 && !F32 ? 3 : 2) void attend_kernel
       if (row < rows) {
         if (whole) {
           const float inv = L == 0.f ? 0.f : 1.f / L;
-          const int tok = row / G;
+          const int tok = token_of(a, row);
           const int qh = head * G + row - tok * G;
           T* out = static_cast<T*>(a.out) + layer * a.out_stride[0] + b * a.out_stride[1] +
                    qh * a.out_stride[2] + tok * a.out_stride[3] + d0;
 #pragma unroll
           for (int v = 0; v < VT; ++v) acc[v] *= inv;
           put_row<VT>(out, acc);
-          if (a.lse && (threadIdx.x & 15) == 0)
+          if (a.lse && (tid & 15) == 0)
             a.lse[(((int64_t)layer * a.n + b) * a.q_heads + qh) * a.q_len + tok] =
                 L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994531f;
         } else {
@@ -678,7 +694,7 @@ __global__ __launch_bounds__(64 * W, RT == 1 && !F32 ? 3 : 2) void attend_kernel
 #pragma unroll
           for (int v = 0; v < VT; v += 4)
             *reinterpret_cast<f32x4*>(po + v) = f32x4{acc[v], acc[v + 1], acc[v + 2], acc[v + 3]};
-          if ((threadIdx.x & 15) == 0) a.part_ml[at] = make_float2(M, L);
+          if ((tid & 15) == 0) a.part_ml[at] = make_float2(M, L);
         }
       }
     }
@@ -766,7 +782,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, uint32_t
     }
   }
   const float inv = L == 0.f ? 0.f : 1.f / L;
-  const int tok = row / a.group;
+  const int tok = token_of(a, row);
   const int qh = head * a.group + row - tok * a.group;
   T* out = static_cast<T*>(a.out) + layer * a.out_stride[0] + b * a.out_stride[1] +
            qh * a.out_stride[2] + tok * a.out_stride[3] + d0;
