@@ -814,11 +814,11 @@ hipError_t launch(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.total == 0) return e;   // one run: nothing to join
   // Pieces of a row: about the runs over the sequences.  A workgroup a row where few rows have
-  // many (32 rows of 96 pieces: 5 us); thousands of rows would be all launch (20000 rows of 9
-  // pieces: 86 us so; of 3 pieces, eight rows a workgroup, 9 us).
+  // many (32 rows of 96 pieces: 5 us); where the rows are many for their pieces it would be all
+  // launch (4096 rows of 8 pieces 24 us, 20000 of 9 86 us; eight rows a workgroup 6 and 9 us).
   constexpr int kRows = 256 / (D / 4);
-  const int64_t rows = a.q_len * a.group;
-  const bool many = a.target >= 8 * (int64_t)a.n && rows * a.c.heads * a.n * a.layers <= 4096;
+  const int64_t rows = a.q_len * a.group, pieces = a.target / a.n;
+  const bool many = pieces >= 8 && rows * a.c.heads * a.n * a.layers <= 32 * pieces;
   const int64_t blocks = many ? rows : (rows + kRows - 1) / kRows;
   const int64_t g2 = blocks * a.c.heads * a.n * a.layers;
   if (g2 * 256 > kMaxThreads) return hipErrorInvalidValue;
