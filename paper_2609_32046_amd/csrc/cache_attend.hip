@@ -381,46 +381,13 @@ __global__ __launch_bounds__(64 * W, RT == 1 && !F32 ? 3 : 2) void attend_kernel
     const int lo = rlo * kRound;   // below 2^31 - 2^16
     const int end = (int64_t)rhi * kRound < len ? rhi * kRound : len;
 
-    // Limits of this lane's rows; the positions that all rows of the tile see, and that any sees.
-    int pr = r;
-    if constexpr (RT > 1) asm volatile("" : "+v"(pr));
-    int limit[RT];
-    const T* qp[RT];
-    bool live[RT];
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      const int row = row0 + t * 16 + pr;
-      live[t] = row < rows;
-      const int tok = live[t] ? token_of(a, row) : 0;
-      const int qh = head * G + (live[t] ? row - tok * G : 0);
-      const int see = a.causal ? len - m + tok + 1 : len;
-      limit[t] = !live[t] || see < 0 ? 0 : see < end ? see : end;
-      qp[t] = static_cast<const T*>(a.q) + layer * a.q_stride[0] + b * a.q_stride[1] +
-              qh * a.q_stride[2] + tok * a.q_stride[3];
-    }
-    // rows ascend with tokens, so the first row sees least, the last live one most
+    // The positions that all rows of the tile see, and that any sees: rows ascend with tokens, so the
+    // first row sees least, the last live one most
     const int row_last = (row0 + RT * 16 < rows ? row0 + RT * 16 : rows) - 1;
     const int see_first = a.causal ? len - m + token_of(a, row0) + 1 : len;
     const int see_last = a.causal ? len - m + token_of(a, row_last) + 1 : len;
     const int full = see_first < end ? (see_first > 0 ? see_first : 0) : end;
     const int hi = see_last < end ? (see_last > 0 ? see_last : 0) : end;
-
-    // before the codes, whose loads the loop keeps under way
-    Query<D, F32> q[kSharedQ ? 1 : RT];
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      if constexpr (kSharedQ) {
-        // held in LDS, in the lanes' order: 16 reads a step of 64 rows, against 64 registers
-        if (t % W == wave) {
-          q[0].load(qp[t], g, live[t]);
-#pragma unroll
-          for (int j = 0; j < KS; ++j) sq[t][j][lane] = q[0].x[j][0];
-        }
-      } else {
-        q[t].load(qp[t], g, live[t]);
-      }
-    }
-    if (kSharedQ) __syncthreads();
 
     const int steps = hi <= lo ? 0 : (hi - lo + kTurn - 1) / kTurn;
     // The page table through the scalar cache: its waits are apart from those for the codes,
@@ -450,6 +417,39 @@ __global__ __launch_bounds__(64 * W, RT == 1 && !F32 ? 3 : 2) void attend_kernel
 #pragma unroll
       for (int i = 0; i < NB - 1; ++i) fetch(i, raw[i]);
     }
+
+    // Limits of this lane's rows.
+    int pr = r;
+    if constexpr (RT > 1) asm volatile("" : "+v"(pr));
+    int limit[RT];
+    const T* qp[RT];
+    bool live[RT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      const int row = row0 + t * 16 + pr;
+      live[t] = row < rows;
+      const int tok = live[t] ? token_of(a, row) : 0;
+      const int qh = head * G + (live[t] ? row - tok * G : 0);
+      const int see = a.causal ? len - m + tok + 1 : len;
+      limit[t] = !live[t] || see < 0 ? 0 : see < end ? see : end;
+      qp[t] = static_cast<const T*>(a.q) + layer * a.q_stride[0] + b * a.q_stride[1] +
+              qh * a.q_stride[2] + tok * a.q_stride[3];
+    }
+    Query<D, F32> q[kSharedQ ? 1 : RT];
+#pragma unroll
+    for (int t = 0; t < RT && steps > 0; ++t) {
+      if constexpr (kSharedQ) {
+        // held in LDS, in the lanes' order: 16 reads a step of 64 rows, against 64 registers
+        if (t % W == wave) {
+          q[0].load(qp[t], g, live[t]);
+#pragma unroll
+          for (int j = 0; j < KS; ++j) sq[t][j][lane] = q[0].x[j][0];
+        }
+      } else {
+        q[t].load(qp[t], g, live[t]);
+      }
+    }
+    if (kSharedQ) __syncthreads();
 
     float top[RT], sum[RT];
     f32x4 o[RT][VT];
