@@ -29,7 +29,7 @@
 // joining.  Many rows are bound by issue: a step of 64 rows is 64 MFMAs (1060 cycles), 32
 // exponentials (380) and about 250 other vector instructions (1150), and the two waves of a
 // SIMD overlap little of it: 2500 rows (500 tokens of 40 heads) over 32768 positions
-// take 356 us, 940 TFLOP/s.  Tried for them and slower: conversions shared through LDS
+// take 354 us, 950 TFLOP/s.  Tried for them and slower: conversions shared through LDS
 // (416-459 us), 32 x 32 x 16 MFMAs (402 us), waves with rows of their own (371 us).
 #include <math.h>
 
@@ -834,22 +834,22 @@ hipError_t launch(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
 // Workgroups resident at a time: 256 compute units, three each of the
 // 16-row kernels, two of the others.
 constexpr int64_t kUnits = 256;
-// Rounds of the shortest run: 16 sequences of 1024 positions take 16.3 us in runs of two
-// rounds, 18.4 of four, 21.8 of eight.
+// Rounds of the shortest run: 16 sequences of 1024 positions in a wide table take 16.3 us in runs
+// of two rounds, 18.4 of four, 21.8 of eight.
 constexpr int64_t kShortest = 2;
 // Where no sequence can be longer than so many rounds, each stays whole, a run of its own, and
 // nothing is joined: kWhole of them where the workgroups are few, up to kWholeFull where they
-// fill half the device.  Decoding over 8 KV heads, cut and whole: one of 1024 positions 14.6 and
-// 11.3 us, of 2048 13.5 and 16.1; 16 of 2048 17.7 and 15.8, of 4096 21.6 and 26.5; 64 of 1024
-// 25.1 and 14.7, of 4096 39.4 and 36.0.  128 tokens of 32 heads behind 300 positions, 64 times:
-// 190 and 138.  Longer ones are cut however many they are: one among many short ones would be
+// fill half the device.  Decoding over 8 KV heads, cut and whole: one of 1024 positions 13.9 and
+// 10.7 us, of 2048 14.0 and 15.6; 16 of 2048 17.5 and 15.7, of 4096 21.8 and 26.3; 64 of 1024
+// 24.5 and 14.2, of 4096 38.5 and 36.1.  128 tokens of 32 heads behind 300 positions, 64 times:
+// 161 and 96.  Longer ones are cut however many they are: one among many short ones would be
 // a single workgroup's work.
 constexpr int64_t kWhole = 8, kWholeFull = 32;
 // And where the waves that the device holds are taken often enough for their length, once for every
 // kAlone rounds, a workgroup is one wave, which has its rows to itself: nothing meets in
-// LDS.  With four waves and with one: 64 times 128 tokens of 32 heads over 300 positions 139 and 70 us,
-// over 1000 188 and 135 (1.3 times for 8 rounds), 20 times over 1000 73 and 67, over
-// 4000 165 and 210; 150 decoding over 256 positions 14.8 and 13.9, over 768 22.4 and 28.1.
+// LDS.  With four waves and with one: 64 times 128 tokens of 32 heads over 300 positions 96 and 55 us,
+// over 1000 143 and 118; 20 times over 1000 57 and 58, over 4000 131 and 191; 8 times over 300 15.7 and
+// 23.1; 150 decoding over 256 positions 14.2 and 13.9, over 768 22.9 and 28.5.
 constexpr int64_t kAlone = 8;
 
 bool make_attend_plan(int layers, int n, int heads, int q_heads, int64_t q_len, int D, bool f32,
