@@ -107,9 +107,18 @@ __device__ inline bool fill_lists(const CacheView& c, SeqList* const (&l)[N],
       most[k] = p > most[k] ? p : most[k];
     }
   }
+  // one lane a wave: the compiler would walk the lanes for an atomic of them all (2 us for 64)
+  if ((int)(threadIdx.x & ~63u) < n) {
 #pragma unroll
-  for (int k = 0; k < N; ++k)
-    if (most[k] > 0) atomicMax(&l[k]->most, most[k]);
+    for (int k = 0; k < N; ++k) {
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const int o = __shfl_xor(most[k], d);
+        most[k] = o > most[k] ? o : most[k];
+      }
+      if ((threadIdx.x & 63) == 0) atomicMax(&l[k]->most, most[k]);
+    }
+  }
   return bad;
 }
 
@@ -121,6 +130,19 @@ __device__ inline void drop(int32_t* refs, int page) {
 // Offsets of the entries' needs, need(i) pages each; returns the total.
 template <typename Need>
 __device__ inline int64_t plan_offsets(PlanShared& sh, int n, Need need) {
+  if (n <= 64) {   // one wave's work, and one barrier
+    if (threadIdx.x < 64) {
+      const int i = threadIdx.x;
+      const int64_t mine = i < n ? need(i) : 0, incl = wave_scan(mine);
+      if (i < n) sh.offset[i] = incl - mine > kCacheMaxPages ? kCacheMaxPages + 1 : (int)(incl - mine);
+      if (i == 63) {
+        sh.offset[n] = incl > kCacheMaxPages ? kCacheMaxPages + 1 : (int)incl;
+        sh.sums[0] = incl;
+      }
+    }
+    __syncthreads();
+    return sh.sums[0];
+  }
   int64_t base = 0;
   for (int i0 = 0; i0 < n; i0 += kPlan) {
     const int i = i0 + threadIdx.x;
@@ -182,12 +204,17 @@ struct Sweep {
   template <typename Take>
   __device__ void give(const PlanShared& sh, int64_t base, int64_t want, Take take) const {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    // the wave's ranks in lanes 0..kScan-1; rows from the wanted ones on are passed over
+    const int first = lane < kScan ? sh.rows[lane * kPlanWaves + wave] : 0;
+    uint64_t todo = __ballot(lane < kScan && base + first < want);
 #pragma unroll 1
-    for (int j = 0; j < kScan; ++j) {
+    while (todo != 0) {
+      const int j = __ffsll((unsigned long long)todo) - 1;
+      todo &= todo - 1;
       const bool is = (free >> j) & 1u;
       const uint64_t b = __ballot(is);
       const int64_t rank =
-          base + sh.rows[j * kPlanWaves + wave] + __popcll(b & ((1ull << lane) - 1));
+          base + __builtin_amdgcn_readlane(first, j) + __popcll(b & ((1ull << lane) - 1));
       if (is && rank < want) take((int)(p0 + j * kPlan), (int)rank);
     }
   }
