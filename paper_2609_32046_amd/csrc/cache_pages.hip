@@ -7,7 +7,7 @@
 // plans in one workgroup (it checks every entry before it changes anything,
 // and takes back what it released when pages lack), then moves bytes with the
 // whole device.  A plan is a chain of reads that wait for one another (list, length, row, count):
-// 9 us to extend 64 sequences, 13 to fork 64 children of 32 pages, 8-10 to compact; giving
+// 5 us to extend 64 sequences, 10 to fork 64 children of 32 pages, 7-8 to compact; giving
 // back 64 sequences takes 5.
 #include "cache.h"
 
