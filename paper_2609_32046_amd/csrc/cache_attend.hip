@@ -834,6 +834,7 @@ hipError_t launch(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
 // Workgroups resident at a time: 256 compute units, three each of the
 // 16-row kernels, two of the others.
 constexpr int64_t kUnits = 256;
+constexpr int64_t kFewSteps = 24;
 // Rounds of the shortest run: 16 sequences of 1024 positions in a wide table take 16.3 us in runs
 // of two rounds, 18.4 of four, 21.8 of eight.
 constexpr int64_t kShortest = 2;
@@ -863,8 +864,14 @@ bool make_attend_plan(int layers, int n, int heads, int q_heads, int64_t q_len, 
   // registers at D = 128.  A call that cannot fill the device takes one block to a wave: more
   // workgroups, each sooner done (32 fp32 rows over 512 positions: 7.2 us, 10.3 with two).
   const int64_t single = (rows + 15) / 16 * heads * layers;
+  // And one of few steps a SIMD takes two blocks rather than four, whose beginning and end weigh
+  // more than the conversions they spare: 256 tokens of 32 heads behind 1024 positions (4 steps of
+  // 64 rows) 14.5 and 21.1 us, 64 behind 8192 (8) 26.4 and 31.8, 32 behind 32768 (16) 37.0 and
+  // 39.2, 64 behind 32768 (32) 57.0 and 53.8.
+  const int64_t steps = (capacity + kStep - 1) / kStep, quads = (rows + 63) / 64;
+  const bool few = quads * units <= kFewSteps * 4 * kUnits / steps;
   p->blocks = rows <= 16 || (f32 && D == 128) || (single <= kUnits && single * most <= kUnits)
-                  ? 1 : rows <= 32 || f32 ? 2 : 4;
+                  ? 1 : rows <= 32 || f32 || few ? 2 : 4;
   const int64_t per = p->blocks * 16;
   const int64_t tiles = (rows + per - 1) / per;
   const int64_t sets = tiles * heads * layers;

@@ -468,6 +468,9 @@ def check_attend(torch, m, q, out, lse, seqs, q_lens, causal, scale, layer0, dty
     scale = scale or 1.0 / math.sqrt(D)
     for l, i in itertools.product(range(Lq), range(n)):
         s, T = seqs[i], q_lens[i]
+        if T <= 0:
+            assert (od[l, i] == fill).all()
+            continue
         length = int(m.lens[s])
         for h in range(m.pool.shape[2]):
             k, v, there = m.read(s, layer0 + l, h)
@@ -549,7 +552,7 @@ def test_attend_single_tokens(torch, cb, dtype, D, P, Hkv, G, cut):
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("D,P,G,m", [(128, 32, 4, 5), (64, 16, 3, 7), (128, 16, 1, 33), (64, 64, 8, 20), (128, 128, 5, 50),
-                                       (64, 16, 7, 40), (128, 32, 8, 65)])
+                                       (64, 16, 7, 40), (128, 32, 8, 65), (64, 16, 8, 65)])
 def test_attend_several_tokens(torch, cb, causal, dtype, D, P, G, m, cut):
     """Prompts' parts: more query tokens than positions (rows of no position), ragged query counts, one
     of none, sequences named out of order and twice, the second layer."""
@@ -606,20 +609,30 @@ def test_attend_scale_and_large_logits(torch, cb):
 @pytest.mark.parametrize("D,P,G,m", [(128, 32, 4, 1), (64, 16, 2, 8), (128, 16, 3, 9), (64, 64, 8, 4), (128, 64, 4, 16),
                                        (64, 32, 5, 25), (128, 128, 8, 17)])
 def test_attend_hundreds_of_short_sequences(torch, cb, dtype, D, P, G, m):
-    """So many that each wave takes rows of its own: 400 entries over eight sequences, most of no or one query
-    token, some of all."""
+    """So many that each wave takes rows of its own: 400 entries over eight sequences."""
+    crowd(torch, cb, dtype, D, P, G, m, 400, [0, 1, 16, 17, 33, 100, 128, 64])
+
+
+@pytest.mark.parametrize("D,P,G,m,n,longest", [(128, 64, 4, 16, 6400, 128), (64, 32, 5, 25, 3200, 128),
+                                                 (128, 64, 4, 16, 400, 2000), (64, 16, 8, 9, 300, 2000)])
+def test_attend_crowds_in_tiles_of_64_rows(torch, cb, D, P, G, m, n, longest):
+    """Enough steps for four blocks a wave: one wave a workgroup, and four over whole sequences."""
+    crowd(torch, cb, "bf16", D, P, G, m, n, [0, 1, 16, 17, 33, 100, longest, 64])
+
+
+def crowd(torch, cb, dtype, D, P, G, m, n, lens):
+    """n entries over eight sequences, most of no or one query token, some of all."""
     rng = np.random.default_rng(m)
-    lens = [0, 1, 16, 17, 33, 100, 128, 64]
-    q_lens = [int(x) for x in rng.choice([0, 0, 0, 1], 400)]
+    q_lens = [int(x) for x in rng.choice([0, 1], n, p=[0.9, 0.1])]
     for i in range(8):
-        q_lens[50 * i + i] = [m, m + 3, (m + 1) // 2][i % 3]
-    attend_case(torch, cb, lens, 1, G, D, P, m, dtype, True, seqs=[i % 8 for i in range(400)], q_lens=q_lens,
+        q_lens[n // 8 * i + i] = [m, m + 3, (m + 1) // 2][i % 3]
+    attend_case(torch, cb, lens, 1, G, D, P, m, dtype, True, seqs=[i % 8 for i in range(n)], q_lens=q_lens,
                 seed=m + G + D)
 
 
-@pytest.mark.parametrize("many", [False, True])
+@pytest.mark.parametrize("rest,cut", [(0, False), (1198, False), (18, True)])
 @pytest.mark.parametrize("dtype,G", [("bf16", 3), ("f32", 3), ("bf16", 20), ("bf16", 30)])
-def test_attend_masked_places_hold_anything(torch, cb, dtype, G, many):
+def test_attend_masked_places_hold_anything(torch, cb, dtype, G, rest, cut):
     """Positions behind the limit with NaN groups, infinite values and any bytes: rows that do not see
     them stay as they are, rows that do are NaN in the group's values (or wholly, for a key)."""
     D, P, lens, m = 128, 32, [75, 40], 12
@@ -639,9 +652,9 @@ def test_attend_masked_places_hold_anything(torch, cb, dtype, G, many):
         q = 38 - 32
         c.pool[int(pages[1, 1]), 0, :, 2 * n + q * 4 + 2] = 255
 
-    rest = 398 if many else 0                     # entries of no query token, beside which a workgroup is one wave
+    # rest: entries of no query token; beside many of them a workgroup is one wave
     _, _, out, _, _ = attend_case(torch, cb, lens, 1, G, D, P, m, dtype, True, seed=11, prepare=spoil,
-                                  seqs=[0, 1] + [0] * rest, q_lens=[m, m] + [0] * rest)
+                                  seqs=[0, 1] + [0] * rest, q_lens=[m, m] + [0] * rest, cut=cut)
     nan = torch.isnan(out[0, 0])                  # [heads][rows][D]
     assert nan[:, 7:, 32:64].all() and not nan[:, :7].any() and not nan[:, 7:, :32].any()
     nan = torch.isnan(out[0, 1])
