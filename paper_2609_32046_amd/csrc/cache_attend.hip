@@ -29,7 +29,7 @@
 // joining.  Many rows are bound by issue: a step of 64 rows is 64 MFMAs (1060 cycles), 32
 // exponentials (380) and about 250 other vector instructions (1150), and the two waves of a
 // SIMD overlap little of it: 2500 rows (500 tokens of 40 heads) over 32768 positions
-// take 354 us, 950 TFLOP/s.  Tried for them and slower: conversions shared through LDS
+// take 350 us, 955 TFLOP/s.  Tried for them and slower: conversions shared through LDS
 // (416-459 us), 32 x 32 x 16 MFMAs (402 us), waves with rows of their own (371 us).
 #include <math.h>
 
