@@ -167,8 +167,8 @@ int cb_rotary(const cb_rows* rows, int32_t parts, int32_t head_dim, const double
       total *= r.size[d] ? r.size[d] : 1;
       if (total > ((int64_t)1 << 40)) return CB_ERR_SHAPE;
     }
-    // a thread for eight values of the rows of one head
-    if (r.size[2] > (cb::kMaxThreads - 255) / (head_dim / 8 + 1)) return CB_ERR_SHAPE;
+    // a thread for eight values of the rows of one head, workgroups of whole rows at least half full
+    if (r.size[2] > (cb::kMaxThreads - 255) / (2 * (head_dim / 8 + 1))) return CB_ERR_SHAPE;
     const bool none = r.size[0] == 0 || r.size[1] == 0 || r.size[2] == 0;
     if (!none && (!r.in || !r.out || !r.pos)) return CB_ERR_NULL;
     if (!aligned(r.in, 16) || !aligned(r.out, 16) || !aligned(r.pos, 4) || !aligned(r.from, 4))

@@ -152,6 +152,20 @@ def test_rotary_sizes(torch, cb):
     check_rotary(torch, big, want, freq, np.array([[[1, 2, 3]]]), 1.0, False, False, "bf16")
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D,R,T", [(1024, 8, 5), (1024, 1022, 40), (1024, 512, 9), (64, 16, 700), (64, 38, 301), (128, 70, 130),
+                                     (72, 72, 257), (8, 2, 1000), (128, 64, 1)])
+def test_rotary_parts_of_many_rows(torch, cb, dtype, D, R, T):
+    """Rows over several workgroups, of one row and of many, with more turned or more copied pieces."""
+    freq, amp = cb.cb_rotary_frequencies(R, 1e4)
+    fd = torch.tensor(freq, dtype=torch.float64, device="cuda")
+    x = randn(torch, D + R, 1, 2, T, D).to(dt(torch, dtype)).cuda()
+    y, pos = torch.full_like(x, 7.0), torch.arange(T, dtype=torch.int32, device="cuda")
+    cb.cb_rotary(cb.rows(x, y, pos), fd, amp)
+    check_rotary(torch, y, x, freq, np.arange(T) * np.ones((1, 2, T)), amp, False, False, dtype)
+    assert torch.equal(y[..., R:], x[..., R:])
+
+
 def test_rotary_refuses_tensors(torch, cb):
     x, p = torch.zeros((1, 1, 2, 8), device="cuda"), ints(torch, [0, 1])
     f = torch.zeros(4, dtype=torch.float64, device="cuda")
