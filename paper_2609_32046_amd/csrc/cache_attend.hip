@@ -334,7 +334,10 @@ __global__ __launch_bounds__(64 * W, RT == 1 && !F32 ? 3 : 2) void attend_kernel
   constexpr int KS = D / 32;              // first product: MFMAs of a block and half
   constexpr int VT = D / 16;              // second: tiles of 16 values
   constexpr int NQ = F32 ? 3 : 1;
-  constexpr int NB = RT == 1 && !F32 ? 3 : 2;     // steps of codes in registers, all but one under way
+  // Steps of codes in registers, the next under way.  With three the loop is half as long again, which a
+  // short sequence pays in instruction fetches: 131072 positions 31.1 us, 29.7 with two; 512
+  // positions 7.7 and 7.0.
+  constexpr int NB = 2;
   constexpr bool kSharedQ = !F32 && RT > 1;       // the four waves' query rows are the same
   constexpr int kPad = 4;
   constexpr int kTurn = kStep * W;                // positions of a workgroup's step
@@ -466,18 +469,17 @@ __global__ __launch_bounds__(64 * W, RT == 1 && !F32 ? 3 : 2) void attend_kernel
       if (t0 >= hi) return;
       const bool masked = t0 + kStep > full || cur.here != 3u;   // uniform
       uint32_t vs[2] = {cur.vs[0], cur.vs[1]};
-      uint32_t nan_bits = 0;   // positions of the lane whose value group reads as NaN
+      uint32_t nans[2] = {0u, 0u};   // 0x80 in the byte of a position whose value group reads as NaN
       if (masked) {
         // what a masked position holds counts for nothing: 0 times a NaN or an
         // infinity would be NaN
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int pos = t0 + (i >> 2) * 16 + 4 * g + (i & 3);
-          const bool in = pos < hi && ((cur.here >> (i >> 2)) & 1u);
-          const uint32_t field = 255u << (8 * (i & 3));
-          const bool nan = (vs[i >> 2] & field) == field;
-          if (in && nan) nan_bits |= 1u << i;
-          if (!in || nan) vs[i >> 2] &= ~field;
+        for (int h = 0; h < 2; ++h) {
+          const int left = ((cur.here >> h) & 1u) ? hi - (t0 + 16 * h + 4 * g) : 0;   // of the lane's four
+          const uint32_t keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
+          const uint32_t y = ~vs[h];   // a byte of zero where the scale is 255
+          nans[h] = ~(((y & 0x7f7f7f7fu) + 0x7f7f7f7fu) | y | 0x7f7f7f7fu) & keep;
+          vs[h] &= keep & ~((nans[h] >> 7) * 255u);
         }
       }
       float vscale[8];
@@ -569,13 +571,13 @@ __global__ __launch_bounds__(64 * W, RT == 1 && !F32 ? 3 : 2) void attend_kernel
                 __builtin_amdgcn_mfma_f32_16x16x32_bf16(odd, p[t][u], o[t][2 * v + 1], 0, 0, 0);
           }
       }
-      if (masked && __any(nan_bits != 0)) {
+      if (masked && __any((nans[0] | nans[1]) != 0u)) {
         // a value that reads as NaN reaches the rows that see its position, in its group
         constexpr int kRun = 16 / (D / 32);               // lanes r of one group
         const int r0 = (g * (D / 32) / 4) * kRun;         // the group that this lane's outputs lie in
 #pragma unroll 1
         for (int i = 0; i < 8; ++i) {
-          const uint64_t who = __ballot((nan_bits >> i) & 1u);
+          const uint64_t who = __ballot(((i < 4 ? nans[0] : nans[1]) >> (8 * (i & 3) + 7)) & 1u);
 #pragma unroll 1
           for (int gg = 0; gg < 4; ++gg) {
             const int pos = t0 + (i >> 2) * 16 + 4 * gg + (i & 3);
