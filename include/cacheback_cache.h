@@ -206,7 +206,8 @@ int cb_cache_read(const cb_cache* c, int32_t layer0, int32_t layers, const int32
  * with CB_F32 in 24 bits.  A position without a page counts for nothing.
  * longest: what the caller knows of the lengths: sequences longer than this are
  * taken to be this long (0: as long as the table allows).  Short sequences in a
- * wide table are faster with it: none is cut, and no results are joined.
+ * wide table are faster with it: none is cut, and no results are joined.  n times
+ * its multiples of 128 positions have to stay below 2^31 (CB_ERR_SHAPE).
  * ws: cb_cache_attend_workspace_bytes bytes (same `longest`), 16-byte aligned;
  * its contents need not be initialised.  Deterministic.  At most two kernels. */
 size_t cb_cache_attend_workspace_bytes(const cb_cache* c, int32_t layers, int32_t n,

@@ -120,7 +120,7 @@ __device__ inline int token_of(const AttendArgs& a, int row) {
 __device__ inline int rounds_of(int len) { return len <= kRound ? 1 : (len + kRound - 1) / kRound; }
 
 // Sum over the lanes.
-__device__ inline int64_t wave_sum64(int64_t x) {
+__device__ inline uint32_t wave_sum(uint32_t x) {
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) x += __shfl_xor(x, d);
   return x;
@@ -128,38 +128,36 @@ __device__ inline int64_t wave_sum64(int64_t x) {
 
 // The same value in scalar registers, where every lane holds the same.
 __device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ inline int64_t uniform64(int64_t x) {
-  return (int64_t)(((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32) | (uint32_t)uniform((int)x));
-}
 
-// Where run `run` of `runs` begins: a sequence and the rounds before it (of all sequences).
-// *per: rounds a run.  False behind the last.  Every wave works it out for itself.
+// Where run `run` begins: a sequence and the rounds before it (of all sequences), all of them
+// below 2^31.  Every wave works it out for itself.
 struct Run {
   int b;
-  int64_t before, lo, hi;   // rounds before sequence b; the run
+  uint32_t before, lo, hi;   // rounds before sequence b; the run
 };
 
-__device__ inline int64_t rounds_per_run(const AttendArgs& a, int64_t* total) {
-  int64_t t = 0;
+__device__ inline uint32_t rounds_per_run(const AttendArgs& a, uint32_t* total) {
+  uint32_t t = 0;
   if (a.n == 1) {
     t = rounds_of(uniform_len(a, 0));
   } else {
     for (int i = threadIdx.x & 63; i < a.n; i += 64) t += rounds_of(seq_len(a, i));
-    t = wave_sum64(t);
+    t = wave_sum(t);
   }
-  t = uniform64(t);
+  t = uniform(t);
   *total = t;
-  return (t + a.target - 1) / a.target;
+  return (t + a.target - 1) / (uint32_t)a.target;
 }
 
+// False behind the last run.
 __device__ inline bool find_run(const AttendArgs& a, int run, Run* r) {
   if (a.whole) {   // a run a sequence
-    *r = {run, 0, 0, rounds_of(uniform_len(a, run))};
+    *r = {run, 0, 0, (uint32_t)rounds_of(uniform_len(a, run))};
     return true;
   }
-  int64_t total;
-  const int64_t per = rounds_per_run(a, &total);
-  r->lo = run * per;
+  uint32_t total;
+  const uint32_t per = rounds_per_run(a, &total);
+  r->lo = run * per;   // below total + target
   r->hi = r->lo + per < total ? r->lo + per : total;
   r->b = 0;
   r->before = 0;
@@ -168,21 +166,21 @@ __device__ inline bool find_run(const AttendArgs& a, int run, Run* r) {
   const int lane = threadIdx.x & 63;
   for (int i0 = 0; i0 < a.n; i0 += 64) {
     const int i = i0 + lane;
-    const int64_t k = i < a.n ? rounds_of(seq_len(a, i)) : 0;
-    int64_t incl = k;
+    const uint32_t k = i < a.n ? rounds_of(seq_len(a, i)) : 0;
+    uint32_t incl = k;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
-      const int64_t y = __shfl_up(incl, d);
+      const uint32_t y = __shfl_up(incl, d);
       if (lane >= d) incl += y;
     }
     const uint64_t mine = __ballot(r->before + incl > r->lo);
     if (mine) {
       const int l = __ffsll((unsigned long long)mine) - 1;
       r->b = i0 + uniform(l);
-      r->before += uniform64(__shfl(incl - k, l));
+      r->before += uniform(__shfl(incl - k, l));
       return true;
     }
-    r->before += uniform64(__shfl(incl, 63));
+    r->before += uniform(__shfl(incl, 63));
   }
   return false;
 }
@@ -372,7 +370,7 @@ __global__ __launch_bounds__(64 * W, RT == 1 && !F32 ? 3 : 2) void attend_kernel
     const int b = run.b;
     const int seq = seq_of(a, b);
     const int len = uniform_len(a, b);
-    const int64_t before = run.before;
+    const uint32_t before = run.before;
     const int rounds = rounds_of(len);
     run.before += rounds;
     const int m = query_tokens(a, b);
@@ -725,14 +723,14 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, uint32_t
   const int rows = query_tokens(a, b) * a.group;
   const bool live = row < rows;
   if (SETS > 1 && !live) return;   // one row a workgroup
-  int64_t total;
-  const int64_t per = rounds_per_run(a, &total);
-  int64_t before = 0;
+  uint32_t total;
+  const uint32_t per = rounds_per_run(a, &total);
+  uint32_t before = 0;
   if (b > 0) {
     for (int i = (int)threadIdx.x & 63; i < b; i += 64) before += rounds_of(seq_len(a, i));
-    before = uniform64(wave_sum64(before));
+    before = uniform(wave_sum(before));
   }
-  const int64_t first = before / per;
+  const uint32_t first = before / per;
   const int count = (int)((before + rounds_of(uniform_len(a, b)) - 1) / per - first) + 1;
   if (count == 1 || !live) return;
   const int d0 = ((int)threadIdx.x % kLanes) * 4;
@@ -893,6 +891,7 @@ bool make_attend_plan(int layers, int n, int heads, int q_heads, int64_t q_len, 
   }
   if (target > most) target = most;
   const int64_t longest = (capacity + kRound - 1) / kRound, groups = sets * n;
+  if (n * longest > 0x7fffffff) return false;   // rounds are counted in 32 bits
   p->whole = longest <= kWholeFull && groups * kThreads <= kMaxThreads &&
              longest <= kWhole + (kWholeFull - kWhole) * groups / (resident / 2);
   if (p->whole) target = n;

@@ -232,6 +232,9 @@ def test_calls_refuse_sizes_past_a_launch(cb):
     need = cb._lib.cb_cache_attend_workspace_bytes
     assert need(many, 4096, 2**20, 4096, 2**26, 0) == need(long, 2, 2**20, 4, 64, 0) == 0
     assert f["attend"](c, scale=3e38) == -2
+    far = L(desc(cb, width=2**27 - 4096))                      # 2^24 rounds of 128 positions
+    assert f["attend"](far, seqs=FAKE, n=200, m=1) == -2 and need(far, 2, 200, 4, 1, 0) == 0
+    assert need(far, 2, 200, 4, 1, 2**20) > 0
 
 
 def test_status_refuses(cb):
