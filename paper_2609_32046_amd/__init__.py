@@ -669,7 +669,7 @@ def _cache_rows(fn, where, c, k, v, seqs, start, counts, layer, stream):
     dev, s = _cache_now(c, where, stream)
     kind, shape = _float_kind(k, where), k.shape
     if len(shape) != 5 or shape[2] != c.kv_heads or shape[4] != c.head_dim or v.shape != shape or \
-            max(shape) > 0x7fffffff or not 0 <= layer < 4096:
+            (shape[0] | shape[1] | shape[2]) >> 31 or not 0 <= layer < 4096:
         _refuse(where, v, f"rows [layers][n][{c.kv_heads}][rows][{c.head_dim}] are wanted, keys and "
                           f"values alike, {tuple(shape)} at layer {layer} given")
     if v.dtype is not k.dtype:
@@ -710,7 +710,7 @@ def cb_cache_attend(c: cb_cache, q, out, ws=None, lse=None, seqs=None, q_lens=No
     dev, s = _cache_now(c, where, stream)
     kind, shape = _float_kind(q, where), q.shape
     if len(shape) != 5 or shape[4] != c.head_dim or out.shape != shape or \
-            max(shape) > 0x7fffffff or not 0 <= layer < 4096:
+            (shape[0] | shape[1] | shape[2]) >> 31 or not 0 <= layer < 4096:
         _refuse(where, out, f"rows [layers][n][q_heads][q_len][{c.head_dim}] and their like are wanted, "
                             f"{tuple(shape)} at layer {layer} given")
     if out.dtype is not q.dtype:

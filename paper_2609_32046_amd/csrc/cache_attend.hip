@@ -24,12 +24,12 @@
 // is a sequence and the second kernel falls away; where there are many, a workgroup is one
 // wave and nothing meets at all.
 //
-// Few rows are bound by HBM: 64 sequences of up to 16384 positions (606 MB) take 121 us in all,
-// 5.0 TB/s, against 109 us with the loads alone; one of 131072 (143 MB) takes 31 us and 5 us of
+// Few rows are bound by HBM: 64 sequences of up to 16384 positions (606 MB) take 118 us in all,
+// 5.1 TB/s, against 109 us with the loads alone; one of 131072 (143 MB) takes 30 us and 5 us of
 // joining.  Many rows are bound by issue: a step of 64 rows is 64 MFMAs (1060 cycles), 32
 // exponentials (380) and about 250 other vector instructions (1150), and the two waves of a
 // SIMD overlap little of it: 2500 rows (500 tokens of 40 heads) over 32768 positions
-// take 350 us, 955 TFLOP/s.  Tried for them and slower: conversions shared through LDS
+// take 351 us, 950 TFLOP/s.  Tried for them and slower: conversions shared through LDS
 // (416-459 us), 32 x 32 x 16 MFMAs (402 us), waves with rows of their own (371 us).
 #include <math.h>
 
