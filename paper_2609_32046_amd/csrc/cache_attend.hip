@@ -24,8 +24,8 @@
 // is a sequence and the second kernel falls away; where there are many, a workgroup is one
 // wave and nothing meets at all.
 //
-// Few rows are bound by HBM: 64 sequences of up to 16384 positions (606 MB) take 118 us in all,
-// 5.1 TB/s, against 109 us with the loads alone; one of 131072 (143 MB) takes 30 us and 5 us of
+// Few rows are bound by HBM: 64 sequences of up to 16384 positions (606 MB) take 117 us in all,
+// 5.2 TB/s, against 109 us with the loads alone; one of 131072 (143 MB) takes 28 us and 5 us of
 // joining.  Many rows are bound by issue: a step of 64 rows is 64 MFMAs (1060 cycles), 32
 // exponentials (380) and about 250 other vector instructions (1150), and the two waves of a
 // SIMD overlap little of it: 2500 rows (500 tokens of 40 heads) over 32768 positions
@@ -709,7 +709,7 @@ template <int D, bool F32, int SETS>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, uint32_t row_blocks) {
   typedef typename RowType<F32>::type T;
   constexpr int kLanes = D / 4, kRows = 256 / kLanes / SETS;
-  constexpr int kAhead = SETS > 1 ? 12 : 4;   // pieces under way: 96 runs of a row in one turn
+  constexpr int kAhead = SETS > 1 ? 12 : 4;   // pieces under way: 96 of a row in one turn
   __shared__ f32x4 so[SETS][kLanes];
   __shared__ float2 sml[SETS];
   uint32_t id = blockIdx.x;
@@ -814,7 +814,7 @@ hipError_t launch(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.total == 0) return e;   // one run: nothing to join
   // Pieces of a row: about the runs over the sequences.  A workgroup a row where few rows have
-  // many (32 rows of 96 pieces: 5 us); where the rows are many for their pieces it would be all
+  // many (32 rows of 64 pieces: 5 us); where the rows are many for their pieces it would be all
   // launch (4096 rows of 8 pieces 24 us, 20000 of 9 86 us; eight rows a workgroup 6 and 9 us).
   constexpr int kRows = 256 / (D / 4);
   const int64_t rows = a.q_len * a.group, pieces = a.target / a.n;
@@ -831,8 +831,10 @@ hipError_t launch(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
 
 }  // namespace
 
-// Workgroups resident at a time: 256 compute units, three each of the
-// 16-row kernels, two of the others.
+// Workgroups at a time: 256 compute units with two each, and with three of the 16-row kernels at
+// D = 64, whose steps are half the bytes: 64 sequences up to 16384 positions at D = 64 take 71.5 us
+// so and 73.6 with two; at D = 128 one of 32768 takes 16.0 us with three and 15.4 with two, its fp32 form 20.8
+// and 17.3 (fewer pieces to join).
 constexpr int64_t kUnits = 256;
 constexpr int64_t kFewSteps = 24;
 // Rounds of the shortest run: 16 sequences of 1024 positions in a wide table take 16.3 us in runs
@@ -840,9 +842,9 @@ constexpr int64_t kFewSteps = 24;
 constexpr int64_t kShortest = 2;
 // Where no sequence can be longer than so many rounds, each stays whole, a run of its own, and
 // nothing is joined: kWhole of them where the workgroups are few, up to kWholeFull where they
-// fill half the device.  Decoding over 8 KV heads, cut and whole: one of 1024 positions 13.9 and
-// 10.7 us, of 2048 14.0 and 15.6; 16 of 2048 17.5 and 15.7, of 4096 21.8 and 26.3; 64 of 1024
-// 24.5 and 14.2, of 4096 38.5 and 36.1.  128 tokens of 32 heads behind 300 positions, 64 times:
+// fill half the device.  Decoding over 8 KV heads, cut and whole: one of 1024 positions 13.4 and
+// 10.2 us, of 2048 13.5 and 15.1; 16 of 2048 16.7 and 15.1, of 4096 19.2 and 26.3; 64 of 1024
+// 20.2 and 13.4, of 4096 35.2 and 35.4.  128 tokens of 32 heads behind 300 positions, 64 times:
 // 161 and 96.  Longer ones are cut however many they are: one among many short ones would be
 // a single workgroup's work.
 constexpr int64_t kWhole = 8, kWholeFull = 32;
@@ -850,7 +852,7 @@ constexpr int64_t kWhole = 8, kWholeFull = 32;
 // kAlone rounds, a workgroup is one wave, which has its rows to itself: nothing meets in
 // LDS.  With four waves and with one: 64 times 128 tokens of 32 heads over 300 positions 96 and 55 us,
 // over 1000 143 and 118; 20 times over 1000 57 and 58, over 4000 131 and 191; 8 times over 300 15.7 and
-// 23.1; 150 decoding over 256 positions 14.2 and 13.9, over 768 22.9 and 28.5.
+// 23.1; 150 decoding over 256 positions 12.8 and 12.8, over 512 17.0 and 20.2.
 constexpr int64_t kAlone = 8;
 
 bool make_attend_plan(int layers, int n, int heads, int q_heads, int64_t q_len, int D, bool f32,
@@ -875,7 +877,7 @@ bool make_attend_plan(int layers, int n, int heads, int q_heads, int64_t q_len, 
   const int64_t per = p->blocks * 16;
   const int64_t tiles = (rows + per - 1) / per;
   const int64_t sets = tiles * heads * layers;
-  const int64_t resident = kUnits * (p->blocks == 1 ? 3 : 2);
+  const int64_t resident = kUnits * (p->blocks == 1 && D == 64 ? 3 : 2);
   // Workgroups run in rounds of `resident`: the number of runs that leaves least of the last
   // one idle, the pieces of a further run counting for a fiftieth.
   int64_t target = 1;
@@ -895,7 +897,8 @@ bool make_attend_plan(int layers, int n, int heads, int q_heads, int64_t q_len, 
   p->whole = longest <= kWholeFull && groups * kThreads <= kMaxThreads &&
              longest <= kWhole + (kWholeFull - kWhole) * groups / (resident / 2);
   if (p->whole) target = n;
-  p->alone = p->whole && longest * kWaves * resident <= kAlone * groups;
+  const int64_t waves = kWaves * kUnits * (p->blocks == 1 ? 3 : 2);   // that the device holds
+  p->alone = p->whole && longest * waves <= kAlone * groups;
   const bool joins = target > 1 && !p->whole;
   p->room = (int32_t)capacity;   // below 2^31 - 2^16
   p->row_tiles = (int32_t)tiles;
