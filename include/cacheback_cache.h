@@ -202,8 +202,10 @@ int cb_cache_read(const cb_cache* c, int32_t layer0, int32_t layers, const int32
  * left as they are.  lse (nullable) [layers][n][q_heads][q_len] fp32:
  * ln sum_t exp(scale * q . K[t]), -inf for a row of no position.  scale: >= 0,
  * 0 selects 1/sqrt(D).  dtype of q and out: CB_F32 or CB_BF16; logits, statistics
- * and sums in fp32; with CB_BF16 the weights enter the product with V in bf16,
- * with CB_F32 in 24 bits.  A position without a page counts for nothing.
+ * and sums in fp32.  The weights enter the product with V in 24 bits with CB_F32.  With
+ * CB_BF16 they enter in 16 bits where q_len * q_heads / kv_heads is at most 16, and
+ * for more query rows in 16 or in 8 (each off by at most 2^-8 of itself).  A position
+ * without a page counts for nothing.
  * longest: what the caller knows of the lengths: sequences longer than this are
  * taken to be this long (0: as long as the table allows).  Short sequences in a
  * wide table are faster with it: none is cut, and no results are joined.  n times

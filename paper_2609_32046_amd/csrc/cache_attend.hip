@@ -14,7 +14,7 @@
 // Codes become bf16 by conversion with their scale, exactly.  (A scaled MFMA that takes
 // the codes as they are, with the query in two fp8 parts, spares the keys' conversions,
 // but sums with about 16 bits: log-sums were off by 2e-5.)  fp32 queries and weights go
-// in as three bf16 parts, 24 bits.
+// in as three bf16 parts, 24 bits; the weights of bf16 calls as two or one (kernel).
 //
 // The positions of all sequences, in rounds of 128, are dealt to the workgroups in
 // equal runs, however ragged they are: a run may end one sequence and begin the next
@@ -332,6 +332,13 @@ __global__ __launch_bounds__(64 * W, RT == 1 && !F32 ? 3 : 2) void attend_kernel
   constexpr int KS = D / 32;              // first product: MFMAs of a block and half
   constexpr int VT = D / 16;              // second: tiles of 16 values
   constexpr int NQ = F32 ? 3 : 1;
+  // bf16 parts of a weight.  Two, 16 bits, where a wave holds one block: outputs are then as near as
+  // their own rounding lets them be (0.0016 of their size over thousands of positions; 0.0023 with one part)
+  // for 0 to 4% of the time of a call (131072 positions 31.7 and 32.1 us, 64 sequences up to 16384 121.5 and
+  // 122.0), 7 or 8% where a wave has few steps (16 of 2048: 16.0 and 17.3; 16 tokens of 32 heads behind 1024
+  // 9.9 and 10.5).  With more rows the products weigh more: 2500 rows
+  // over 32768 positions take 354 us with one part and 490 with two, 32 tokens of 32 heads 34.6 and 40.3.
+  constexpr int NW = F32 ? 3 : RT == 1 ? 2 : 1;
   // Steps of codes in registers, the next under way.  With three the loop is half as long again, which a
   // short sequence pays in instruction fetches: 131072 positions 31.1 us, 29.7 with two; 512
   // positions 7.7 and 7.0.
@@ -484,7 +491,7 @@ __global__ __launch_bounds__(64 * W, RT == 1 && !F32 ? 3 : 2) void attend_kernel
 #pragma unroll
       for (int i = 0; i < 8; ++i)
         vscale[i] = __uint_as_float(((vs[i >> 2] >> (8 * (i & 3))) & 255u) << 23);
-      bf16x8 p[RT][NQ];
+      bf16x8 p[RT][NW];
       {
         bf16x8 kk[2][KS];
 #pragma unroll
@@ -547,12 +554,18 @@ __global__ __launch_bounds__(64 * W, RT == 1 && !F32 ? 3 : 2) void attend_kernel
 #pragma unroll
             for (int u = 0; u < 3; ++u) p[t][u] = __builtin_bit_cast(bf16x8, w[u]);
           } else {
-            // the weights' rounding: at most 2^-9 of each, in either direction, under
-            // the rounding of the bf16 output itself
-            u32x4 w;
+            // the rounding of a weight: at most 2^-8 of it, as much as an output's own; what is
+            // left of it, rounded again, leaves 2^-16
+            u32x4 w, lo;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = pack_bf16(e[2 * i], e[2 * i + 1]);
+            for (int i = 0; i < 4; ++i) {
+              w[i] = pack_bf16(e[2 * i], e[2 * i + 1]);
+              if constexpr (NW == 2)
+                lo[i] = pack_bf16(e[2 * i] - __uint_as_float(w[i] << 16),
+                                  e[2 * i + 1] - __uint_as_float(w[i] & 0xffff0000u));
+            }
             p[t][0] = __builtin_bit_cast(bf16x8, w);
+            if constexpr (NW == 2) p[t][1] = __builtin_bit_cast(bf16x8, lo);
           }
         }
       }
@@ -563,7 +576,7 @@ __global__ __launch_bounds__(64 * W, RT == 1 && !F32 ? 3 : 2) void attend_kernel
 #pragma unroll
         for (int t = 0; t < RT; ++t)
 #pragma unroll
-          for (int u = NQ - 1; u >= 0; --u) {
+          for (int u = NW - 1; u >= 0; --u) {
             o[t][2 * v] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(even, p[t][u], o[t][2 * v], 0, 0, 0);
             o[t][2 * v + 1] =
                 __builtin_amdgcn_mfma_f32_16x16x32_bf16(odd, p[t][u], o[t][2 * v + 1], 0, 0, 0);
