@@ -93,7 +93,9 @@ int cb_rotary(const cb_rows* rows, int32_t parts, int32_t head_dim, const double
  * clamped to -124..125; a value is held as the nearest of 0, 0.5, 1, 1.5, 2,
  * 3, 4, 6 times the scale (ties to the even code, larger ones to 6) and its
  * sign: bit 3 of the code.  What a code stands for is exact in bf16.  A group
- * with a NaN or an infinity gets the byte 255, and all of it reads as NaN.
+ * with a NaN or an infinity gets the byte 255, and all of it reads as NaN.  The bytes
+ * 253 and 254 are never stored: what a group that holds one, in a page's unwritten
+ * positions say, reads as is not defined (its values, infinities or NaN).
  *
  * pool  [pages][layers][kv_heads][unit] bytes, unit = P * (D + D/16) for the
  *       P = page_len positions of a page:

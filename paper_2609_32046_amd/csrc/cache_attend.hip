@@ -474,16 +474,17 @@ __global__ __launch_bounds__(64 * W, RT == 1 && !F32 ? 3 : 2) void attend_kernel
       if (t0 >= hi) return;
       const bool masked = t0 + kStep > full || cur.here != 3u;   // uniform
       uint32_t vs[2] = {cur.vs[0], cur.vs[1]};
-      uint32_t nans[2] = {0u, 0u};   // 0x80 in the byte of a position whose value group reads as NaN
+      uint32_t nans[2] = {0u, 0u};   // 0x80 in the byte of a position whose value group may not be finite
       if (masked) {
-        // what a masked position holds counts for nothing: 0 times a NaN or an
-        // infinity would be NaN
+        // what a masked position holds counts for nothing: 0 times a NaN or an infinity would be
+        // NaN.  A scale of 255 is NaN, with 253 and 254 (never stored, but a page may hold anything
+        // before its positions are written) codes pass bf16's range.
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const int left = ((cur.here >> h) & 1u) ? hi - (t0 + 16 * h + 4 * g) : 0;   // of the lane's four
           const uint32_t keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
-          const uint32_t y = ~vs[h];   // a byte of zero where the scale is 255
-          nans[h] = ~(((y & 0x7f7f7f7fu) + 0x7f7f7f7fu) | y | 0x7f7f7f7fu) & keep;
+          // bytes of 253 and up: bit 7 is set, and the seven below reach 125
+          nans[h] = ((vs[h] & 0x7f7f7f7fu) + 0x03030303u) & vs[h] & 0x80808080u & keep;
           vs[h] &= keep & ~((nans[h] >> 7) * 255u);
         }
       }
@@ -583,7 +584,7 @@ __global__ __launch_bounds__(64 * W, RT == 1 && !F32 ? 3 : 2) void attend_kernel
           }
       }
       if (masked && __any((nans[0] | nans[1]) != 0u)) {
-        // a value that reads as NaN reaches the rows that see its position, in its group
+        // a value that is not finite reaches the rows that see its position, as NaN in its group
         constexpr int kRun = 16 / (D / 32);               // lanes r of one group
         const int r0 = (g * (D / 32) / 4) * kRun;         // the group that this lane's outputs lie in
 #pragma unroll 1

@@ -85,3 +85,38 @@ def test_many_bf16_rows_round_their_weights_apart(torch, cb, D, P, G, m, lens):
         tol = 7.5 * UB * np.sqrt((p * p) @ (v * v)) + p @ np.abs(v) * (2 * err + len(p[0]) / 128 + 56) * U
         tol = tol + UB * (np.abs(want) + tol)
         assert (np.abs(got - want) <= tol).all(), float((np.abs(got - want) / tol).max())
+
+
+# ---- attention: what masked places hold ------------------------------------------
+
+
+@pytest.mark.parametrize("rest,cut", [(0, False), (1198, False), (18, True)])
+@pytest.mark.parametrize("dtype,D,P,G", [("bf16", 128, 32, 1), ("f32", 128, 16, 1), ("bf16", 64, 16, 3), ("f32", 64, 32, 3),
+                                         ("bf16", 128, 64, 20), ("bf16", 64, 64, 30)])
+def test_attend_rows_that_do_not_see_a_position_do_not_feel_it(torch, cb, dtype, D, P, G, rest, cut):
+    """Room for eight positions, four of them not yet written, under a causal mask: the first four query tokens
+    have the same bits whatever bytes the pages hold there."""
+    lens, m = [75, 40], 8
+    c = cache_with(torch, cb, lens, H=2, D=D, P=P, seed=70, width=8192 // P if cut else None)
+    fill_cache(torch, cb, c, lens, 71)
+    # rest: entries of no query token; beside many of them a workgroup is one wave
+    seqs, q_lens = ints(torch, [0, 1] + [0] * rest), ints(torch, [m, m] + [0] * rest)
+    q = randn(torch, 72, 1, 2 + rest, 2 * G, m, D).to(dt(torch, dtype)).cuda()
+    ws = scratch(torch, cb, c, q)
+    table, n, s = c.table.cpu().numpy(), P * D // 2, P * D // 32
+    want = None
+    for k, byte in [(127, 127), (127, 252), (127, 253), (127, 254), (127, 255), (253, 127), (254, 254), (255, 253)]:
+        for i, length in enumerate(lens):
+            for pos in range(length - 4, length):
+                u, at = c.pool[int(table[i, pos // P]), 0], pos % P
+                u[:, at * (D // 2):(at + 1) * (D // 2)] = 0x7F           # 6 and -6
+                u[:, 2 * n + at * (D // 32):2 * n + (at + 1) * (D // 32)] = k
+                u[:, n:2 * n].view(2, P // 4, 16, 4, D // 32)[:, at // 4, :, at % 4] = 0xF7
+                u[:, 2 * n + s:].view(2, P // 4, D // 32, 4)[:, at // 4, :, at % 4] = byte
+        out, lse = torch.full_like(q, 7.0), torch.full(q.shape[:4], 7.0, device="cuda")
+        cb.cb_cache_attend(c.desc, q, out, ws, lse, seqs, q_lens)
+        got = out[:, :2, :, :4].clone(), lse[:, :2, :, :4].clone()
+        if want is None:
+            want = got
+            assert torch.isfinite(got[0]).all() and torch.isfinite(got[1]).all()
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), (k, byte)
