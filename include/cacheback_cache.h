@@ -154,7 +154,8 @@ int cb_cache_free(const cb_cache* c, const int32_t* seqs, int32_t n, void* strea
  * the same full pages and a copy of the page that the last positions fill in
  * part (so that each side can append); copy != 0: a copy of every page.  Pages
  * that a child held before are given back first.  All or nothing; invalid: an
- * entry outside the table, a child listed twice or that is also a parent.
+ * entry outside the table, a child listed twice or that is also a parent, a parent
+ * whose table row does not name a page for each of its positions.
  * n <= 2048.  ws: cb_cache_fork_workspace_bytes(c, n) bytes, 16-byte aligned. */
 size_t cb_cache_fork_workspace_bytes(const cb_cache* c, int32_t n);
 int cb_cache_fork(const cb_cache* c, const int32_t* parents, const int32_t* children, int32_t n,
@@ -165,7 +166,7 @@ int cb_cache_fork(const cb_cache* c, const int32_t* parents, const int32_t* chil
  *   idx[i * idx_stride[0] + l * idx_stride[1] + h * idx_stride[2] + j]
  * of src[i] in that layer and head: codes and scales are moved as they are
  * (strides of 0 use one list for all layers or heads).  A position outside the
- * sequence gives a row of zeros.  dst[i] = src[i] thins a sequence itself; pages
+ * sequence, or without a page, gives a row of zeros.  dst[i] = src[i] thins a sequence itself; pages
  * that dst[i] held before are given back.  The rest of the last page is cleared.
  * All or nothing; invalid: an entry outside the table, a dst listed twice or
  * that is the src of another entry, a count below 0 or over keep.

@@ -360,9 +360,12 @@ __global__ __launch_bounds__(kPlan) void cache_fork_kernel(CacheView c,
   extern __shared__ uint32_t bits[];
   __shared__ PlanShared sh;
   __shared__ SeqList from, to;
+  // A parent's row names what is no page.  Not sh.bad: a wave may find that out while
+  // another still reads sh.bad for the entries.
+  __shared__ int no_page;
   clear_bits(bits, c.seqs);
   if (threadIdx.x == 0) {
-    sh.bad = from.most = to.most = 0;
+    sh.bad = no_page = from.most = to.most = 0;
     *count = 0;
   }
   __syncthreads();
@@ -380,7 +383,7 @@ __global__ __launch_bounds__(kPlan) void cache_fork_kernel(CacheView c,
   }
   // every page that a parent says it holds is one
   each_page(c, from, n, [&](int, int, int p) {
-    if (!is_page(c, p)) sh.bad = 1;
+    if (!is_page(c, p)) no_page = 1;
   });
   auto hold = [&](int d) {   // the children's pages
     each_page(c, to, n, [&](int, int, int p) {
@@ -394,17 +397,18 @@ __global__ __launch_bounds__(kPlan) void cache_fork_kernel(CacheView c,
     return copy ? held_pages(c, len) : (len > 0 && (len & part) != 0);
   });
   __syncthreads();
+  const bool refused = no_page != 0;
   // the children's own pages, and what is copied into them
-  const int64_t have = sh.bad ? -1 : take_free(c, sh, want, [&](int page, int rank) {
+  const int64_t have = refused ? 0 : take_free(c, sh, want, [&](int page, int rank) {
     const int i = entry_of(sh, n, rank);
     const int j = copy ? rank - sh.offset[i] : held_pages(c, from.len[i]) - 1;
     pairs[rank] = make_int2(c.table[(int64_t)from.seq[i] * c.width + j], page);
     c.table[(int64_t)to.seq[i] * c.width + j] = page;
     c.refs[page] = 1;
   });
-  if (have < want) {
+  if (refused || have < want) {
     hold(1);
-    if (threadIdx.x == 0) *status = have < 0 ? -1 : lacking(want - have);
+    if (threadIdx.x == 0) *status = refused ? -1 : lacking(want - have);
     return;
   }
   // the shared ones, and what the children held beyond their new lengths

@@ -120,3 +120,55 @@ def test_attend_rows_that_do_not_see_a_position_do_not_feel_it(torch, cb, dtype,
             want = got
             assert torch.isfinite(got[0]).all() and torch.isfinite(got[1]).all()
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), (k, byte)
+
+
+# ---- pages -----------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("copy", [False, True])
+@pytest.mark.parametrize("n", [1, 3, 64, 65, 200, 1100])
+@pytest.mark.parametrize("entry", [-1, -7, 10**6, 2**31 - 1])
+def test_fork_of_a_parent_without_one_of_its_pages_changes_nothing(torch, cb, entry, n, copy):
+    """A hole, or a number that is no page, anywhere in any parent's row: refused, and the children keep what
+    they held; put right, the same call is done."""
+    P, D = 16, 64
+    lens = [7 * P + 5, 2 * P, 9] + [P + 3] * n
+    c = cache_with(torch, cb, lens, L=1, H=1, D=D, P=P, extra=9 * n, width=9, seed=n)
+    parents, children = ints(torch, [i % 3 for i in range(n)]), ints(torch, list(range(3, 3 + n)))
+    ws = torch.empty(cb.cb_cache_fork_workspace_bytes(c.desc, n), dtype=torch.uint8, device="cuda")
+    for s, j in [(0, 0), (0, 7), (1, 1), (2, 0)]:
+        if s >= n:   # no parent of this call
+            continue
+        before = c.table[s, j].item()
+        c.table[s, j] = entry
+        m = model(c, D, P)
+        c.status.fill_(5)
+        cb.cb_cache_fork(c.desc, parents, children, c.status, ws, copy)
+        assert c.status.item() == -1 and cb.cb_cache_status(c.status) == -2
+        same_state(c, m)
+        c.table[s, j] = before
+    m = model(c, D, P)
+    cb.cb_cache_fork(c.desc, parents, children, c.status, ws, copy)
+    assert c.status.item() == m.fork([i % 3 for i in range(n)], list(range(3, 3 + n)), copy) == 0
+    same_state(c, m)
+
+
+@pytest.mark.parametrize("D,P", [(64, 16), (128, 64)])
+def test_compact_of_positions_without_a_page(torch, cb, D, P):
+    """Kept positions in a hole of the table, or behind an entry that is no page, are rows of zeros."""
+    lens = [4 * P + 3, 10]
+    c = cache_with(torch, cb, lens, L=1, H=2, D=D, P=P, extra=12, width=6)
+    fill_cache(torch, cb, c, lens, 80)
+    c.table[0, 1], c.table[0, 3] = -1, c.pool.shape[0]
+    keep = 4 * P + 3
+    idx = torch.arange(keep, dtype=torch.int32, device="cuda").reshape(1, 1, 1, keep)
+    ws = torch.empty(cb.cb_cache_compact_workspace_bytes(c.desc, 1), dtype=torch.uint8, device="cuda")
+    m = model(c, D, P)
+    cb.cb_cache_compact(c.desc, ints(torch, [0]), ints(torch, [1]), idx, c.status, ws)
+    assert cb.cb_cache_status(c.status) == 0
+    got = model(c, D, P)
+    for h in range(2):
+        k, v, there = m.read(0, 0, h)
+        kk, vv, _ = got.read(1, 0, h)
+        assert np.array_equal(there, [t // P not in (1, 3) for t in range(keep)])
+        assert np.array_equal(kk, k * there[:, None]) and np.array_equal(vv, v * there[:, None])
