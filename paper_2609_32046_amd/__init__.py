@@ -674,8 +674,8 @@ def _cache_rows(fn, where, c, k, v, seqs, start, counts, layer, stream):
                           f"values alike, {tuple(shape)} at layer {layer} given")
     if v.dtype is not k.dtype:
         _refuse(where, v, f"{k.dtype} is wanted", -3)
-    st = _row_strides(k, where, dev)
-    if _row_strides(v, where, dev) != st:
+    st, sv = _row_strides(k, where, dev), _row_strides(v, where, dev)
+    if st != sv and any(a != b and size > 1 for a, b, size in zip(st, sv, shape)):   # of axes that are walked
         _refuse(where, v, "keys and values of unlike strides")
     n = shape[1]
     _check(fn(_byref(c), layer, shape[0], _ints(seqs, where, dev, n), n, _ints(start, where, dev, n),

@@ -172,3 +172,30 @@ def test_compact_of_positions_without_a_page(torch, cb, D, P):
         kk, vv, _ = got.read(1, 0, h)
         assert np.array_equal(there, [t // P not in (1, 3) for t in range(keep)])
         assert np.array_equal(kk, k * there[:, None]) and np.array_equal(vv, v * there[:, None])
+
+
+# ---- sizes and strides of one ------------------------------------------------------
+
+
+@pytest.mark.parametrize("n,H", [(3, 2), (1, 4), (2, 1)])
+def test_rows_of_unlike_strides_along_axes_of_one(torch, cb, n, H):
+    """A decoding step's keys head-major and its values token-major: one token, so every row lies where the
+    other's strides say; with two tokens, or heads apart, it does not, and the call is refused."""
+    D, P = 128, 16
+    c = cache_with(torch, cb, [20] * n, H=H, D=D, P=P)
+    k = randn(torch, 90, 1, n, H, 1, D).bfloat16().cuda()
+    v = randn(torch, 91, n, 1, H, D).bfloat16().cuda().transpose(1, 2)[None]
+    v = v.as_strided(v.shape, (7, *v.stride()[1:3], 5 * D, 1))
+    assert v.shape == k.shape and v.stride() != k.stride()
+    cb.cb_cache_write(c.desc, k, v)
+    ko = torch.zeros_like(k)
+    vo = torch.zeros((n, 1, H, D), dtype=torch.bfloat16, device="cuda").transpose(1, 2)[None]
+    vo = vo.as_strided(v.shape, v.stride())
+    cb.cb_cache_read(c.desc, ko, vo, start=ints(torch, [19] * n))
+    assert np.array_equal(ref.to_f64(ko), ref.values(*ref.quantise(ref.to_f64(k))))
+    assert np.array_equal(ref.to_f64(vo), ref.values(*ref.quantise(ref.to_f64(v))))
+    k2, v2 = torch.zeros((1, n, 2, 2, D), device="cuda"), torch.zeros((1, n, 2, 2, D), device="cuda").transpose(2, 3)
+    c2 = cache_with(torch, cb, [20] * n, H=2, D=D, P=P)
+    for fn in (cb.cb_cache_write, cb.cb_cache_read):
+        with pytest.raises(cb.CBError, match="unlike strides"):
+            fn(c2.desc, k2, v2)
