@@ -81,7 +81,8 @@ typedef struct cb_rows {
  * input given the gradient of the output.  freq: device, R/2 doubles, 8-byte
  * aligned.  Angles are formed in 64 bits, rotations in fp32, each value
  * rounded once to dtype (CB_F32, CB_BF16).  D = head_dim: a multiple of 8,
- * 8..1024, R even, 2..D.  Rows of an output must not overlap one another. */
+ * 8..1024, R even, 2..D.  A tensor has at most 2^40 rows.  Rows of an output must not
+ * overlap one another. */
 int cb_rotary(const cb_rows* rows, int32_t parts, int32_t head_dim, const double* freq,
               int32_t rotary_dim, double amplitude, int32_t interleaved, int32_t transpose,
               int32_t dtype, void* stream);

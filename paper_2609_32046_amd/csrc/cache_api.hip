@@ -161,11 +161,12 @@ int cb_rotary(const cb_rows* rows, int32_t parts, int32_t head_dim, const double
   cb::RotaryArgs a{};
   for (int i = 0; i < parts; ++i) {
     const cb_rows& r = rows[i];
-    int64_t total = 1;
+    int64_t total = 1;   // of rows, at most 2^40; compared by division, as the product may pass 64 bits
     for (int d = 0; d < 3; ++d) {
       if (r.size[d] < 0 || r.size[d] > 0x7fffffff) return CB_ERR_SHAPE;
-      total *= r.size[d] ? r.size[d] : 1;
-      if (total > ((int64_t)1 << 40)) return CB_ERR_SHAPE;
+      const int64_t size = r.size[d] ? r.size[d] : 1;
+      if (size > ((int64_t)1 << 40) / total) return CB_ERR_SHAPE;
+      total *= size;
     }
     // a thread for eight values of the rows of one head, workgroups of whole rows at least half full
     if (r.size[2] > (cb::kMaxThreads - 255) / (2 * (head_dim / 8 + 1))) return CB_ERR_SHAPE;
