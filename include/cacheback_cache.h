@@ -132,7 +132,9 @@ size_t cb_cache_page_bytes(const cb_cache* c);
 /* The lists of sequences below (seqs, parents, ...) are device int32 arrays
  * of n entries.  Where a call says "all or nothing", *status (device,
  * 4-byte aligned) receives 0 when it was done, the number of pages lacking, or
- * -1 for an invalid entry; unless it is 0 the cache is as it was before.
+ * -1 for an invalid entry; unless it is 0 the cache is as it was before.  A call
+ * says what became of it alone, over whatever *status held: calls that rest on one
+ * another (a fork of what was extended) want a word each, or a look between them.
  * New pages are the free pages of lowest number, in the order of the entries. */
 
 /* Synchronises `stream` and says what *status holds: CB_OK, CB_ERR_PAGES, or

@@ -6,6 +6,8 @@ from __future__ import annotations
 
 import itertools
 import math
+import os
+import re
 
 import numpy as np
 import pytest
@@ -199,3 +201,36 @@ def test_rows_of_unlike_strides_along_axes_of_one(torch, cb, n, H):
     for fn in (cb.cb_cache_write, cb.cb_cache_read):
         with pytest.raises(cb.CBError, match="unlike strides"):
             fn(c2.desc, k2, v2)
+
+
+# ---- the documents' example ----------------------------------------------------------
+
+
+def readme_example():
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    text = open(os.path.join(root, "README.md")).read()
+    blocks = [b for b in re.findall(r"```python\n(.*?)```", text, re.S) if "cb_cache_fork" in b]
+    assert len(blocks) == 1
+    return blocks[0]
+
+
+def test_the_example_of_the_readme(torch, cb):
+    got = {}
+    exec(readme_example(), got)
+    c, q, out = got["c"], got["q"], got["out"]
+    assert c.lens.tolist() == [1000, 1000, 1000, 0]
+    m = model(c, got["D"], 64)
+    for l, i, h in [(0, 0, 0), (1, 1, 31)]:
+        k, v, there = m.read(1 + i, l, h // 4)
+        x = ref.to_f64(q[l, i, h, 0])
+        want, _, err, size, _ = ref.attend(x, k, v, 1000, there, 1 / math.sqrt(got["D"]))
+        tol = size * (2.0 ** -16 + (2 * err + 64) * U) + UB * (np.abs(want) + size * 2.0 ** -15)
+        assert (np.abs(ref.to_f64(out[l, i, h, 0]) - want) <= tol).all()
+
+
+def test_the_example_of_the_readme_says_when_pages_lack(torch, cb):
+    """A message of 16 pages and room for 8: nothing is held, so nothing may be answered from it."""
+    text = readme_example()
+    assert "pages=64" in text
+    with pytest.raises(AssertionError):
+        exec(text.replace("pages=64", "pages=8"), {})
