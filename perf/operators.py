@@ -639,6 +639,7 @@ def _handle(st):
             n = cb.cb_cache_attend_workspace_bytes(h, c["L"], c["n"], c["Hq"], c["m"])
         elif c["kind"] == "fork":
             n = cb.cb_cache_fork_workspace_bytes(h, c["parents"] * c["each"])
+            st["forked"] = torch.empty_like(st["status"])   # the extension has a word of its own
         elif c["kind"] == "thin":
             n = cb.cb_cache_compact_workspace_bytes(h, c["n"])
         st["ws"] = torch.empty(n, dtype=torch.uint8, device=DEV) if n else None
@@ -667,7 +668,7 @@ def _own(st):
         return [st["k_out"], st["v_out"]]
     if c["kind"] == "fork":
         cb.cb_cache_free(h, st["children"])
-        cb.cb_cache_fork(h, st["parents"], st["children"], st["status"], st["ws"], copy=c["copy"])
+        cb.cb_cache_fork(h, st["parents"], st["children"], st["forked"], st["ws"], copy=c["copy"])
         cb.cb_cache_extend(h, st["children"], st["add"], st["status"])
     else:
         cb.cb_cache_compact(h, st["src"], st["dst"], st["idx"], st["status"], st["ws"])
