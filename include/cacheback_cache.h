@@ -18,7 +18,8 @@
  * Strided tensors: row strides are given in elements, outermost first; the D
  * values of a row are contiguous, and every row starts on a 16-byte boundary
  * (pointers and strides; CB_ERR_ALIGN otherwise).  A size of zero launches
- * nothing.  Outputs must not overlap inputs unless a call says so.  Sizes that pass
+ * nothing but what writes a call's status.  Outputs must not overlap inputs unless a
+ * call says so.  Sizes that pass
  * the limits named at a call, or one launch's (2^32 - 1 threads along an axis: eight
  * values a thread for rows, 16 to 64 query rows a workgroup for attention), give
  * CB_ERR_SHAPE.
@@ -113,7 +114,7 @@ int cb_rotary(const cb_rows* rows, int32_t parts, int32_t head_dim, const double
  * _compact or _free; cb_cache_write writes where it is told.
  */
 typedef struct cb_cache {
-  int32_t layers, kv_heads;
+  int32_t layers, kv_heads;   /* 1..4096 each */
   int32_t head_dim;   /* D: 64 or 128 */
   int32_t page_len;   /* P: 16, 32, 64, 128 or 256 */
   int32_t pages;      /* 1..2^24 */
@@ -211,13 +212,16 @@ int cb_cache_read(const cb_cache* c, int32_t layer0, int32_t layers, const int32
  * and sums in fp32.  The weights enter the product with V in 24 bits with CB_F32.  With
  * CB_BF16 they enter in 16 bits where q_len * q_heads / kv_heads is at most 16, and
  * for more query rows in 16 or in 8 (each off by at most 2^-8 of itself).  A position
- * without a page counts for nothing.
+ * without a page counts for nothing.  Logits within +-2^28 and values within +-2^60
+ * give finite rows; a row that sees larger ones may come out infinite or NaN.
  * longest: what the caller knows of the lengths: sequences longer than this are
  * taken to be this long (0: as long as the table allows).  Short sequences in a
  * wide table are faster with it: none is cut, and no results are joined.  n times
- * its multiples of 128 positions have to stay below 2^31 (CB_ERR_SHAPE).
+ * its multiples of 128 positions have to stay below 2^31, n is at most 2^20, and q_len and
+ * the query rows of a KV head, q_len * q_heads / kv_heads, at most 2^26 (CB_ERR_SHAPE).
  * ws: cb_cache_attend_workspace_bytes bytes (same `longest`), 16-byte aligned;
- * its contents need not be initialised.  Deterministic.  At most two kernels. */
+ * its contents need not be initialised (0 bytes: no scratch is needed, or the call refuses
+ * the sizes).  Deterministic.  At most two kernels. */
 size_t cb_cache_attend_workspace_bytes(const cb_cache* c, int32_t layers, int32_t n,
                                        int32_t q_heads, int64_t q_len, int64_t longest);
 int cb_cache_attend(const cb_cache* c, int32_t layer0, int32_t layers, const int32_t* seqs,

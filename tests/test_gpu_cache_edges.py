@@ -203,6 +203,130 @@ def test_rows_of_unlike_strides_along_axes_of_one(torch, cb, n, H):
             fn(c2.desc, k2, v2)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_rows_in_pages_of_128(torch, cb, dtype, D):
+    """Codes and scales byte for byte over the borders of pages of 128 positions, everything else as it was."""
+    P, lens, start, T = 128, [300, 128, 5], [100, 0, 1], 150
+    c = cache_with(torch, cb, lens, L=2, H=2, D=D, P=P, seed=D)
+    m = model(c, D, P)
+    counts = [T, 128, 4]
+    k, v = (randn(torch, 95 + i, 1, 3, 2, T, D).to(dt(torch, dtype)).cuda() for i in range(2))
+    cb.cb_cache_write(c.desc, k, v, start=ints(torch, start), counts=ints(torch, counts), layer=1)
+    for x, which in ((k, 0), (v, 1)):
+        code, scale = ref.quantise(ref.to_f64(x))
+        for i, h in itertools.product(range(3), range(2)):
+            for page in range(start[i] // P, (start[i] + counts[i] - 1) // P + 1):
+                u = list(ref.unpack(m.pool[m.table[i, page], 1, h], P, D))
+                a, b = max(start[i], page * P), min(start[i] + counts[i], (page + 1) * P)
+                u[2 * which][a - page * P:b - page * P] = code[0, i, h, a - start[i]:b - start[i]]
+                u[2 * which + 1][a - page * P:b - page * P] = scale[0, i, h, a - start[i]:b - start[i]]
+                m.pool[m.table[i, page], 1, h] = ref.pack(*u)
+    same_state(c, m)
+    ko, vo = torch.full_like(k, 3.0), torch.full_like(v, 3.0)
+    cb.cb_cache_read(c.desc, ko, vo, start=ints(torch, start), counts=ints(torch, counts), layer=1)
+    for x, o in ((k, ko), (v, vo)):
+        want = ref.values(*ref.quantise(ref.to_f64(x)))
+        for i in range(3):
+            assert np.array_equal(ref.to_f64(o[0, i, :, :counts[i]]), want[0, i, :, :counts[i]])
+            assert (o[0, i, :, counts[i]:] == 3.0).all()
+
+
+# ---- attention: large logits ---------------------------------------------------------
+
+
+@pytest.mark.parametrize("cut", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D,P,G,m", [(128, 32, 4, 1), (64, 16, 5, 7), (64, 64, 8, 40)])
+@pytest.mark.parametrize("size", [2.0 ** 10, 2.0 ** 20, 2.0 ** 24, 2.0 ** 28])
+def test_attend_logits_of_any_size(torch, cb, size, D, P, G, m, dtype, cut):
+    """Logits of 6000, of millions and of 2^24 * 12, exact by construction (one value of a key times a power of
+    two), so that one position has all the weight: its values come out, rounded like any product with 1 / sum
+    (2 U, the reciprocal and the product; three parts of a weight 2 U more) and to bf16, and the log-sum is its logit.
+    2^28 * 12 is past the 2^28 that a call answers for: in units of log2 its reference has steps of 512, and half a
+    step in an exponent is past 2^128.  Only rows that see no such logit are looked at."""
+    lens = [333, 200, 40]
+    c = cache_with(torch, cb, lens, H=1, D=D, P=P, width=8192 // P if cut else None)
+    rng = np.random.default_rng(D + m)
+    T = max(lens)
+    k = np.zeros((1, 3, 1, T, D), np.float32)
+    k[0, :2, 0, :, 5] = rng.choice([0.5, -1, 2, 3, -3, 4, -4], (2, T))
+    k[0, 2, 0, :, 5] = rng.choice([-4, -6], T)                     # all logits below zero where size is above
+    at = {0: (321, 17), 1: (3, 180), 2: (30, 11)}                  # of the largest and the smallest
+    k[0, 0, 0, 321, 5], k[0, 0, 0, 17, 5] = 6, -6
+    k[0, 1, 0, 3, 5], k[0, 1, 0, 180, 5] = 6, -6
+    k[0, 2, 0, 30, 5], k[0, 2, 0, 11, 5] = -3, -12
+    v = randn(torch, 96, 1, 3, 1, T, D)
+    cb.cb_cache_write(c.desc, torch.from_numpy(k).cuda(), v.cuda(), start=ints(torch, [0] * 3), counts=ints(torch, lens))
+    q = randn(torch, 97, 1, 3, G, m, D)                            # against zeros: no matter
+    sign = torch.from_numpy(rng.choice([-1.0, 1.0], (1, 3, G, m))).float()
+    q[..., 5] = size * sign
+    q = q.to(dt(torch, dtype)).cuda()
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:4], device="cuda")
+    cb.cb_cache_attend(c.desc, q, out, scratch(torch, cb, c, q), lse, causal=False, scale=1.0)
+    mm = model(c, D, P)
+    for i in range(3):
+        kk, vv, _ = mm.read(i, 0, 0)
+        for g, r in itertools.product(range(G), range(m)):
+            w = at[i][0 if sign[0, i, g, r] > 0 else 1]
+            top = size * sign[0, i, g, r].item() * kk[w, 5]
+            if abs(size * kk[:, 5]).max() > 2.0 ** 28:
+                continue
+            assert top == max(size * sign[0, i, g, r].item() * kk[:, 5]) and (kk[:, 5] == kk[w, 5]).sum() == 1
+            want = vv[w]
+            tol = np.abs(want) * (4 * U + (UB * 1.01 if dtype == "bf16" else 0))
+            assert (np.abs(ref.to_f64(out[0, i, g, r]) - want) <= tol).all()
+            # the logit in units of log2: c2, its product, the sum's logarithm, the way back: U each
+            assert abs(lse[0, i, g, r].item() - top) <= 6 * U * abs(top)
+
+
+# ---- pools past 2^32 bytes -------------------------------------------------------------
+
+
+def test_forks_thinning_and_attention_in_a_large_pool(torch, cb):
+    """Pages that lie beyond 4 GB are shared, copied, thinned and attended to as the same pages of a small pool."""
+    L, H, D, P = 32, 8, 128, 256
+    c = cb.Cache(L, H, D, P, 500, 4, 3)                            # 4.5 GB
+    few = cb.Cache(L, H, D, P, 2, 4, 3)
+    few.pool.random_(0, 256)
+    few.pool[..., P * D:] = (few.pool[..., P * D:] & 3) + 124
+    c.pool[485:499] = 1
+    c.pool[[498, 485]] = few.pool
+    few.table[:, :2] = ints(torch, [0, 1])
+    few.lens.fill_(400)
+    c.refs.fill_(1)
+    c.refs[486:496] = 0
+    c.table[0, :2] = ints(torch, [498, 485])
+    c.lens[0] = 400
+    page = c.pool[0].numel()
+    assert 485 * page > 2 ** 32
+    ws = torch.empty(cb.cb_cache_fork_workspace_bytes(c.desc, 1), dtype=torch.uint8, device="cuda")
+    zero = ints(torch, [0])
+    words = [torch.full_like(c.status, 5) for _ in range(3)]
+    cb.cb_cache_fork(c.desc, zero, ints(torch, [1]), words[0], ws, True)
+    cb.cb_cache_fork(c.desc, zero, ints(torch, [2]), words[1], ws)
+    idx = torch.sort(torch.rand((1, L, H, 400), device="cuda").topk(300, dim=-1)[1], dim=-1)[0].to(torch.int32)
+    cw = torch.empty(cb.cb_cache_compact_workspace_bytes(c.desc, 1), dtype=torch.uint8, device="cuda")
+    cb.cb_cache_compact(c.desc, zero, ints(torch, [3]), idx, words[2], cw)
+    assert [w.item() for w in words] == [0, 0, 0]
+    assert c.table.tolist() == [[498, 485, -1], [486, 487, -1], [498, 488, -1], [489, 490, -1]]
+    assert torch.equal(c.pool[[486, 487]], few.pool) and torch.equal(c.pool[[498, 488]], few.pool)
+    got = [torch.empty((L, 1, H, 300, D), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    all_ = [torch.empty((L, 1, H, 400, D), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    cb.cb_cache_read(c.desc, *got, ints(torch, [3]))
+    cb.cb_cache_read(few.desc, *all_, zero)
+    for x, y in zip(got, all_):
+        assert torch.equal(x[:, 0], y[:, 0].gather(2, idx[0].long().unsqueeze(-1).expand(L, H, 300, D)))
+    for m in (1, 30):
+        q = randn(torch, 98, L, 3, 2 * H, m, D).bfloat16().cuda()
+        outs = []
+        for x in (c, few):
+            out = torch.empty_like(q)
+            cb.cb_cache_attend(x.desc, q, out, scratch(torch, cb, x, q), seqs=ints(torch, [0, 1, 2]))
+            outs.append(out)
+        assert torch.isfinite(outs[0]).all() and torch.equal(*outs)
+
+
 # ---- the documents' example ----------------------------------------------------------
 
 
