@@ -186,7 +186,8 @@ int cb_cache_compact(const cb_cache* c, const int32_t* src, const int32_t* dst, 
  * layer0..layer0+layers-1.  Row t < counts[i] (NULL: max_count) goes to
  * position start[i] + t of sequence seqs[i] (NULL: sequence i); start = NULL:
  * the sequence's last counts[i] positions.  A row whose position has no page
- * is passed over.  No position may be written twice in a call. */
+ * is passed over.  counts[i] below 0 is taken as 0, above max_count as max_count.  No
+ * position may be written twice in a call. */
 int cb_cache_write(const cb_cache* c, int32_t layer0, int32_t layers, const int32_t* seqs,
                    int32_t n, const int32_t* start, const int32_t* counts, int64_t max_count,
                    const void* k, const void* v, const int64_t stride[4], int32_t dtype,
@@ -208,8 +209,8 @@ int cb_cache_read(const cb_cache* c, int32_t layer0, int32_t layers, const int32
  * hold.  A row with limit <= 0 gives zeros; query tokens from q_lens[i] on are
  * left as they are.  lse (nullable) [layers][n][q_heads][q_len] fp32:
  * ln sum_t exp(scale * q . K[t]), -inf for a row of no position.  scale: >= 0,
- * 0 selects 1/sqrt(D).  dtype of q and out: CB_F32 or CB_BF16; logits, statistics
- * and sums in fp32.  The weights enter the product with V in 24 bits with CB_F32.  With
+ * 0 selects 1/sqrt(D).  q_lens[i] below 0 is taken as 0, above q_len as q_len.
+ * dtype of q and out: CB_F32 or CB_BF16; logits, statistics and sums in fp32.  The weights enter the product with V in 24 bits with CB_F32.  With
  * CB_BF16 they enter in 16 bits where q_len * q_heads / kv_heads is at most 16, and
  * for more query rows in 16 or in 8 (each off by at most 2^-8 of itself).  A position
  * without a page counts for nothing.  Logits within +-2^28 and values within +-2^60

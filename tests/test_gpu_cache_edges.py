@@ -327,6 +327,177 @@ def test_forks_thinning_and_attention_in_a_large_pool(torch, cb):
         assert torch.isfinite(outs[0]).all() and torch.equal(*outs)
 
 
+# ---- the smallest and the largest calls ------------------------------------------------
+
+
+def test_counts_beyond_the_rows_that_are_given(torch, cb):
+    """More rows named than there are: all of them, the sequence's last; fewer than none: none."""
+    D, P = 64, 16
+    c = cache_with(torch, cb, [40, 33, 20], D=D, P=P)
+    m = model(c, D, P)
+    k = randn(torch, 100, 1, 3, 2, 5, D).cuda()
+    counts = ints(torch, [5, 2**31 - 1, -2**31])
+    cb.cb_cache_write(c.desc, k, k, counts=counts)
+    after = model(c, D, P)
+    want = ref.values(*ref.quantise(ref.to_f64(k)))
+    for s, n in ((0, 40), (1, 33), (2, 20)):
+        for h in range(2):
+            kk, vv, _ = after.read(s, 0, h)
+            ko, vo, _ = m.read(s, 0, h)
+            if s < 2:
+                ko[n - 5:], vo[n - 5:] = want[0, s, h], want[0, s, h]
+            assert np.array_equal(kk, ko, equal_nan=True) and np.array_equal(vv, vo, equal_nan=True)
+    ko, vo = torch.full_like(k, 3.0), torch.full_like(k, 3.0)
+    cb.cb_cache_read(c.desc, ko, vo, counts=counts)
+    assert np.array_equal(ref.to_f64(ko[:, :2]), want[:, :2]) and (ko[:, 2] == 3.0).all() and torch.equal(ko, vo)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_a_cache_of_one_page(torch, cb, D):
+    """One page, one sequence, one layer and head: filled, read, attended to, refused more, given back."""
+    c = cb.Cache(1, 1, D, 16, 1, 1, 1)
+    zero, one = ints(torch, [0]), ints(torch, [1])
+    ws = torch.empty(max(cb.cb_cache_fork_workspace_bytes(c.desc, 1), cb.cb_cache_compact_workspace_bytes(c.desc, 1)),
+                     dtype=torch.uint8, device="cuda")
+    for t in range(16):
+        cb.cb_cache_extend(c.desc, zero, one, c.status)
+        assert c.status.item() == 0 and c.lens.tolist() == [t + 1] and c.refs.tolist() == [1]
+        k, v = randn(torch, 101 + t, 1, 1, 1, 1, D).cuda(), randn(torch, 131 + t, 1, 1, 1, 1, D).cuda()
+        cb.cb_cache_write(c.desc, k, v)
+        q = randn(torch, 161 + t, 1, 1, 1, 1, D).cuda()
+        out = torch.empty_like(q)
+        cb.cb_cache_attend(c.desc, q, out)
+        for got, want, p, vv, err in rows_of(model(c, D, 16), q, out, [0]):
+            assert (np.abs(got - want) <= p @ np.abs(vv) * (2 * err + 56) * U).all()
+    cb.cb_cache_extend(c.desc, zero, one, c.status)
+    assert cb.cb_cache_status(c.status) == -2          # longer than the table
+    idx = torch.zeros((1, 1, 1, 1), dtype=torch.int32, device="cuda")
+    cb.cb_cache_compact(c.desc, zero, zero, idx, c.status, ws)
+    assert c.status.item() == 1 and c.lens.tolist() == [16] and c.refs.tolist() == [1]
+    cb.cb_cache_fork(c.desc, zero, zero, c.status, ws)
+    assert c.status.item() == -1
+    cb.cb_cache_free(c.desc, zero)
+    assert c.lens.tolist() == [0] and c.refs.tolist() == [0] and c.table.tolist() == [[-1]]
+
+
+def test_a_cache_of_the_most_sequences(torch, cb):
+    """2^17 sequences and calls of 2048 entries: the last of each."""
+    n, seqs, P, D = 2048, 1 << 17, 16, 64
+    c = cb.Cache(1, 1, D, P, 3 * n, seqs, 2)
+    m = ref.Model(np.zeros((3 * n, 0)), c.refs.cpu().numpy(), c.table.cpu().numpy(), c.lens.cpu().numpy(), D, P)
+    a, b = list(range(seqs - n, seqs)), list(range(n))
+    add = [1 + i % 17 for i in range(n)]
+    cb.cb_cache_extend(c.desc, ints(torch, a), ints(torch, add), c.status)
+    assert c.status.item() == m.extend(a, add) == 0
+    same_state(c, m, pool=False)
+    for bad in (a[:-1] + [a[0]], a[:-1] + [seqs]):
+        cb.cb_cache_extend(c.desc, ints(torch, bad), ints(torch, add), c.status)
+        assert c.status.item() == -1
+    same_state(c, m, pool=False)
+    m.pool = c.pool.cpu().numpy()
+    ws = torch.empty(cb.cb_cache_fork_workspace_bytes(c.desc, n), dtype=torch.uint8, device="cuda")
+    cb.cb_cache_fork(c.desc, ints(torch, a), ints(torch, b), c.status, ws)
+    assert c.status.item() == m.fork(a, b, False) == 0
+    same_state(c, m)
+    cb.cb_cache_free(c.desc, ints(torch, a + b + a))
+    assert not c.refs.any() and not c.lens.any() and int(c.table.max()) == -1
+
+
+def test_a_pool_of_the_most_pages(torch, cb):
+    """2^24 pages of which only the last few are free: found, taken and given back."""
+    pages = 1 << 24
+    c = cb.Cache(1, 1, 64, 16, pages, 3, 8)
+    c.refs.fill_(1)
+    c.refs[pages - 7:] = 0
+    c.refs[pages - 3] = 1
+    cb.cb_cache_extend(c.desc, ints(torch, [2, 0]), ints(torch, [40, 33]), c.status)
+    assert c.status.item() == 0
+    free = [pages - 7, pages - 6, pages - 5, pages - 4, pages - 2, pages - 1]
+    assert c.table[[2, 0], :4].tolist() == [[*free[:3], -1], [*free[3:], -1]] and int(c.refs.min()) == 1
+    k = randn(torch, 102, 1, 1, 1, 9, 64).cuda()
+    cb.cb_cache_write(c.desc, k, k, ints(torch, [0]))
+    out = torch.empty_like(k)
+    cb.cb_cache_read(c.desc, out, k.clone(), ints(torch, [0]))
+    assert np.array_equal(ref.to_f64(out), ref.values(*ref.quantise(ref.to_f64(k))))
+    cb.cb_cache_extend(c.desc, ints(torch, [1]), ints(torch, [1]), c.status)
+    assert c.status.item() == 1
+    cb.cb_cache_free(c.desc, ints(torch, [0, 2]))
+    assert c.refs[pages - 7:].tolist() == [0, 0, 0, 0, 1, 0, 0]
+
+
+@pytest.mark.parametrize("dtype,causal,G,m", [("f32", True, 2, 1), ("bf16", False, 4, 1), ("bf16", True, 8, 3)])
+def test_a_sequence_of_nearly_2_to_the_31_positions(torch, cb, dtype, causal, G, m):
+    """As long as a table allows, most of its entries one page: the row's weights are those of the page and of
+    the last positions, many times over.  Its sums have 2^26 / (runs * waves) terms a wave, each rounded: at most half
+    a step, and so many of them below 2^18 with 64 runs of four waves; the values of the page's positions
+    add up to nearly nothing against those of the end, which makes the limit seen."""
+    D, P = 64, 256
+    width = ((1 << 31) - (1 << 16)) // P
+    c = cb.Cache(1, 1, D, P, 3, 2, width)
+    length = width * P - 77
+    c.table[0] = 0
+    c.table[0, width - 1] = 2
+    c.lens[0] = length
+    k = 0.3 * randn(torch, 103, 1, 1, 1, P, D)
+    v = randn(torch, 104, 1, 1, 1, P, D)
+    cb.cb_cache_write(c.desc, k.cuda(), v.cuda(), ints(torch, [0]), ints(torch, [0]))
+    k2, v2 = 0.3 * randn(torch, 105, 1, 1, 1, P - 77, D), randn(torch, 106, 1, 1, 1, P - 77, D)
+    k2[..., 3] = 40.0                                        # the last page's positions weigh as much as all others
+    q = randn(torch, 107, 1, 1, G, m, D)
+    q[..., 3] = 4.3
+    cb.cb_cache_write(c.desc, k2.cuda(), v2.cuda(), ints(torch, [0]), ints(torch, [(width - 1) * P]))
+    got = torch.zeros((1, 1, 1, P - 77, D), device="cuda")
+    cb.cb_cache_read(c.desc, got, torch.empty_like(got), ints(torch, [0]))   # the last P - 77 positions
+    assert np.array_equal(ref.to_f64(got), ref.values(*ref.quantise(ref.to_f64(k2))))
+    q = q.to(dt(torch, dtype)).cuda()
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:4], device="cuda")
+    cb.cb_cache_attend(c.desc, q, out, scratch(torch, cb, c, q), lse, ints(torch, [0]), causal=causal)
+    kk, vv = (ref.values(*ref.quantise(ref.to_f64(x[0, 0, 0]))) for x in (k, v))
+    ke, ve = (ref.values(*ref.quantise(ref.to_f64(x[0, 0, 0]))) for x in (k2, v2))
+    many = width - 1
+    for g, r in itertools.product(range(G), range(m)):
+        x = ref.to_f64(q[0, 0, g, r])
+        end = P - 77 - (m - 1 - r if causal else 0)
+        za, zb = kk @ x / math.sqrt(D), ke[:end] @ x / math.sqrt(D)
+        top = max(za.max(), zb.max())
+        wa, wb = many * np.exp(za - top), np.exp(zb - top)
+        z = wa.sum() + wb.sum()
+        want = (wa @ vv + wb @ ve[:end]) / z
+        size = (wa @ np.abs(vv) + wb @ np.abs(ve[:end])) / z
+        err = ((D + 4) / math.sqrt(D) * (np.abs(np.concatenate([kk, ke])) @ np.abs(x)).max() + 2 * abs(top)) * U
+        lost = 2 * err + 2.0 ** 18 * U + (2.0 ** -16 + 0 if dtype == "bf16" and G * m <= 16 else UB if dtype == "bf16" else 0)
+        tol = size * lost + (UB * (np.abs(want) + size * lost) if dtype == "bf16" else 0)
+        assert (np.abs(ref.to_f64(out[0, 0, g, r]) - want) <= tol).all()
+        assert abs(lse[0, 0, g, r].item() - (top + math.log(z))) <= err + 2.0 ** 18 * U + 8 * U * abs(top + math.log(z))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D,G,m,lens", [(64, 1, 3001, [4000]), (128, 128, 1, [700, 50]), (128, 71, 9, [500]), (64, 2, 1500, [1, 900])])
+def test_attend_wide_groups_and_thousands_of_tokens(torch, cb, dtype, D, G, m, lens):
+    """128 query heads a KV head, a group that is no power of two, 3001 query tokens; every row against 64 bits.
+    Tolerances as in check_attend."""
+    c = cache_with(torch, cb, lens, H=1, D=D, P=64)
+    fill_cache(torch, cb, c, lens, 110)
+    q = randn(torch, 111, 1, len(lens), G, m, D).to(dt(torch, dtype)).cuda()
+    out = torch.empty_like(q)
+    cb.cb_cache_attend(c.desc, q, out, scratch(torch, cb, c, q))
+    mm, qd, od = model(c, D, 64), ref.to_f64(q), ref.to_f64(out)
+    for i, T in enumerate(lens):
+        k, v, _ = mm.read(i, 0, 0)
+        for g in range(G):
+            z = qd[0, i, g] @ k.T / math.sqrt(D)
+            err = ((D + 4) / math.sqrt(D) * (np.abs(qd[0, i, g]) @ np.abs(k).T) + 2 * np.abs(z)).max(1, keepdims=True)
+            limit = T - m + np.arange(m)[:, None] + 1
+            z = np.where(np.arange(T) < limit, z, -np.inf)
+            w = np.exp(z - np.where(limit > 0, z.max(1, keepdims=True), 0.0))
+            p = w / np.where(limit > 0, w.sum(1, keepdims=True), 1.0)
+            want, size = p @ v, p @ np.abs(v)
+            tol = size * (2 * err + T / 128 + 56) * U + 2.0 ** -126 * np.abs(v).sum(0)
+            if dtype == "bf16":
+                tol = tol + UB * (size + np.abs(want))
+            assert (np.abs(od[0, i, g] - want) <= tol).all()
+
+
 # ---- the documents' example ----------------------------------------------------------
 
 
