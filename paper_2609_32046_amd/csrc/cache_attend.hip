@@ -24,8 +24,8 @@
 // is a sequence and the second kernel falls away; where there are many, a workgroup is one
 // wave and nothing meets at all.
 //
-// Few rows are bound by HBM: 64 sequences of up to 16384 positions (606 MB) take 117 us in all,
-// 5.2 TB/s, against 109 us with the loads alone; one of 131072 (143 MB) takes 28 us and 5 us of
+// Few rows are bound by HBM: 64 sequences of up to 16384 positions (606 MB) take 119 us in all,
+// 5.1 TB/s, against 109 us with the loads alone; one of 131072 (143 MB) takes 29 us and 5 us of
 // joining.  Many rows are bound by issue: a step of 64 rows is 64 MFMAs (1060 cycles), 32
 // exponentials (380) and about 250 other vector instructions (1150), and the two waves of a
 // SIMD overlap little of it: 2500 rows (500 tokens of 40 heads) over 32768 positions
@@ -340,8 +340,8 @@ __global__ __launch_bounds__(64 * W, RT == 1 && !F32 ? 3 : 2) void attend_kernel
   // over 32768 positions take 354 us with one part and 490 with two, 32 tokens of 32 heads 34.6 and 40.3.
   constexpr int NW = F32 ? 3 : RT == 1 ? 2 : 1;
   // Steps of codes in registers, the next under way.  With three the loop is half as long again, which a
-  // short sequence pays in instruction fetches: 131072 positions 31.1 us, 29.7 with two; 512
-  // positions 7.7 and 7.0.
+  // short sequence pays in instruction fetches: 131072 positions 34.6 us, 32.4 with two; 512
+  // positions 8.2 and 7.4.
   constexpr int NB = 2;
   constexpr bool kSharedQ = !F32 && RT > 1;       // the four waves' query rows are the same
   constexpr int kPad = 4;
@@ -846,27 +846,29 @@ hipError_t launch(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
 }  // namespace
 
 // Workgroups at a time: 256 compute units with two each, and with three of the 16-row kernels at
-// D = 64, whose steps are half the bytes: 64 sequences up to 16384 positions at D = 64 take 71.5 us
-// so and 73.6 with two; at D = 128 one of 32768 takes 16.0 us with three and 15.4 with two, its fp32 form 20.8
-// and 17.3 (fewer pieces to join).
+// D = 64, whose steps are half the bytes: 64 sequences up to 16384 positions at D = 64 take 75.0 us
+// so and 78.2 with two; at D = 128 one of 32768 takes 16.9 us with three and 15.6 with two, its fp32 form 20.9
+// and 16.9 (fewer pieces to join).
 constexpr int64_t kUnits = 256;
 constexpr int64_t kFewSteps = 24;
-// Rounds of the shortest run: 16 sequences of 1024 positions in a wide table take 16.3 us in runs
-// of two rounds, 18.4 of four, 21.8 of eight.
+// Rounds of the shortest run, where a table is short for as many runs as the device holds: one
+// sequence of 4096 positions takes 9.4 us in runs of one round, 9.7 of two, 11.1 of four, 13.1 of eight; one
+// of 8192 11.1, 10.2, 11.2 and 14.1, two of 4096 12.6, 11.7, 13.1 and 14.9.
 constexpr int64_t kShortest = 2;
 // Where no sequence can be longer than so many rounds, each stays whole, a run of its own, and
 // nothing is joined: kWhole of them where the workgroups are few, up to kWholeFull where they
-// fill half the device.  Decoding over 8 KV heads, cut and whole: one of 1024 positions 13.4 and
-// 10.2 us, of 2048 13.5 and 15.1; 16 of 2048 16.7 and 15.1, of 4096 19.2 and 26.3; 64 of 1024
-// 20.2 and 13.4, of 4096 35.2 and 35.4.  128 tokens of 32 heads behind 300 positions, 64 times:
-// 161 and 96.  Longer ones are cut however many they are: one among many short ones would be
-// a single workgroup's work.
+// fill half the device.  Decoding over 8 KV heads, cut and whole: one of 2048 positions 9.4 and
+// 16.4 us; 16 of 1024 13.1 and 11.0, of 4096 21.2 and 28.9; 64 of 1024 20.4 and 16.6, of 4096 60.6 and
+// 56.9.  128 tokens of 32 heads behind up to 300 positions, 64 times: 160 and 59.  On the border, 16 of
+// 2048 (whole) lose a microsecond, 16.3 and 17.4, and one of 1024 two of them in a graph, 8.4 and 10.3, but
+// gains one where the host has one launch less to make, 10.9 and 9.9.  Longer ones are cut however many they
+// are: one among many short ones would be a single workgroup's work.
 constexpr int64_t kWhole = 8, kWholeFull = 32;
 // And where the waves that the device holds are taken often enough for their length, once for every
 // kAlone rounds, a workgroup is one wave, which has its rows to itself: nothing meets in
 // LDS.  With four waves and with one: 64 times 128 tokens of 32 heads over 300 positions 96 and 55 us,
 // over 1000 143 and 118; 20 times over 1000 57 and 58, over 4000 131 and 191; 8 times over 300 15.7 and
-// 23.1; 150 decoding over 256 positions 12.8 and 12.8, over 512 17.0 and 20.2.
+// 23.1; 150 decoding over 256 positions 14.9 and 14.5, over 512 20.6 and 23.4.
 constexpr int64_t kAlone = 8;
 
 bool make_attend_plan(int layers, int n, int heads, int q_heads, int64_t q_len, int D, bool f32,

@@ -17,11 +17,6 @@ constexpr int kThreads = 256;
 constexpr int kHeads = 4;   // rows of one position that a thread turns by the same angles
 constexpr int64_t kStreamBytes = (int64_t)256 << 20;
 
-// A piece of a row: mode 0, half layout with halves of whole vectors of eight: eight pairs
-// from both halves, then copied vectors; 1, interleaved: eight consecutive values; 2, half
-// layout with other halves: up to eight pairs, the upper ones from anywhere, then up to
-// eight copied values.
-//
 // 16 bytes; STREAM: past the caches, for calls that would only flush them.
 template <bool STREAM, typename V, typename T>
 __device__ inline V get16(const T* p) {
@@ -96,6 +91,12 @@ __device__ inline void angle(double delta, double freq, float amplitude, float s
   *sn = __builtin_amdgcn_sinf(r) * (amplitude * sign);
 }
 
+// A piece of a row: mode 0, half layout with halves of whole vectors of eight: eight pairs
+// from both halves, then copied vectors; 1, interleaved: eight consecutive values; 2, half
+// layout with other halves: up to eight pairs, the upper ones from anywhere, then up to
+// eight copied values.  Mode 2 is the slow one: its upper halves and copied values begin off any
+// vector's border, and its last pairs are stored one by one.  2048 moved keys with 70 of 128 bf16 values
+// turned (302 MB) take 103 us, with 64 of them 55; 38 of 64 fp32 values 94.
 template <typename T, int MODE, bool STREAM>
 struct Turn {
   static constexpr int PAIRS = MODE == 1 ? 4 : 8;
