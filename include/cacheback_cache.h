@@ -170,8 +170,9 @@ int cb_cache_fork(const cb_cache* c, const int32_t* parents, const int32_t* chil
  *   idx[i * idx_stride[0] + l * idx_stride[1] + h * idx_stride[2] + j]
  * of src[i] in that layer and head: codes and scales are moved as they are
  * (strides of 0 use one list for all layers or heads).  A position outside the
- * sequence, or without a page, gives a row of zeros.  dst[i] = src[i] thins a sequence itself; pages
- * that dst[i] held before are given back.  The rest of the last page is cleared.
+ * sequence, or without a page, gives a row of zeros.  dst[i] = src[i] thins a
+ * sequence itself; pages that dst[i] held before are given back.  The rest of the
+ * last page is cleared.
  * All or nothing; invalid: an entry outside the table, a dst listed twice or
  * that is the src of another entry, a count below 0 or over keep.
  * 1 <= keep <= width * page_len, n <= 2048. */
@@ -210,10 +211,11 @@ int cb_cache_read(const cb_cache* c, int32_t layer0, int32_t layers, const int32
  * left as they are.  lse (nullable) [layers][n][q_heads][q_len] fp32:
  * ln sum_t exp(scale * q . K[t]), -inf for a row of no position.  scale: >= 0,
  * 0 selects 1/sqrt(D).  q_lens[i] below 0 is taken as 0, above q_len as q_len.
- * dtype of q and out: CB_F32 or CB_BF16; logits, statistics and sums in fp32.  The weights enter the product with V in 24 bits with CB_F32.  With
- * CB_BF16 they enter in 16 bits where q_len * q_heads / kv_heads is at most 16, and
- * for more query rows in 16 or in 8 (each off by at most 2^-8 of itself).  A position
- * without a page counts for nothing.  Logits within +-2^28 and values within +-2^60
+ * dtype of q and out: CB_F32 or CB_BF16; logits, statistics and sums in fp32.  The
+ * weights enter the product with V in 24 bits with CB_F32.  With CB_BF16 they enter in
+ * 16 bits where q_len * q_heads / kv_heads is at most 16, and for more query rows in 16
+ * or in 8 (each off by at most 2^-8 of itself).  A position without a page counts for
+ * nothing.  Logits within +-2^28 and values within +-2^60
  * give finite rows; a row that sees larger ones may come out infinite or NaN.
  * longest: what the caller knows of the lengths: sequences longer than this are
  * taken to be this long (0: as long as the table allows).  Short sequences in a
